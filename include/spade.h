@@ -19,6 +19,9 @@
  *   spade_verify_qkv_rope   the verify block's QKV projection with rotary
  *                           embedding, writing its K/V into the cache slots
  *                           the attention reads
+ *   The verify step in 4 bits (4-bit weights and a paged 4-bit cache):
+ *   spade_linear_w4, spade_verify_qk_norm_rope_kv4, spade_verify_attention_kv4,
+ *   spade_kv_commit_kv4, spade_kv_read_kv4
  *
  * Conventions shared by every call
  *  - Every pointer argument is a DEVICE pointer owned by the caller; the
@@ -438,6 +441,126 @@ spade_status spade_verify_qkv_rope_paged(const void *x, const void *w_qkv, const
                                          int32_t max_pages, int32_t max_k, float rope_theta,
                                          void *workspace, size_t workspace_bytes, int32_t *status,
                                          spade_stream_t stream);
+
+/* ------------------------------------------------------------------------ */
+/* The verify step in 4 bits                                                 */
+/* ------------------------------------------------------------------------ */
+/*
+ * Weights and a paged KV cache held in 4 bits, for verifiers whose memory holds
+ * more contexts than bf16 caches would, and whose steps are bound by the bytes of
+ * their weights.  A number is
+ *   value = scale * (code - zero),   code in 0 .. 15,
+ * with one pair (scale, zero) of float16 per group of neighbouring numbers; zero is
+ * a whole number in 0 .. 15, so that 0 is held exactly.  Eight neighbouring codes
+ * share a little-endian 32-bit word: bits 4p .. 4p + 3 hold number
+ * (0, 2, 4, 6, 1, 3, 5, 7)[p] of the eight, so that a mask of 4 bits in each half
+ * of the word picks two neighbours.
+ *
+ * The cache:
+ *   k_codes, v_codes    uint8   [num_pages, Hkv, page_size, D / 2], 16-byte aligned
+ *   k_params, v_params  float16 [num_pages, Hkv, page_size, D / 64, 2], 16-byte
+ *                       aligned: (scale, zero) of each group of 64 dims
+ *   block_table         int32 [B, max_pages], as for the other paged calls
+ * D in {64, 128}; page_size a multiple of 64; a sequence's capacity is max_pages *
+ * page_size slots.  How a group x of a key or value head is stored: lo = min(x, 0),
+ * hi = max(x, 0), scale = (hi - lo) / 15 rounded to float16 (at most 4364, so that
+ * every value is in float16's range), zero = round(-lo / scale) cut to 15, code =
+ * round(x / scale) + zero cut to 0 .. 15; a group whose scale rounds to 0 (spans
+ * under 4.5e-7) is held as zeros, one that spans over 65460 is cut.  A group with a value that is not finite gets scale NaN, and with it
+ * every row that attends to the slot.
+ */
+
+/*
+ * y = x W^T (+ residual), rounded to bf16 once: a projection with 4-bit weights
+ * (the verifier's linear layers in x_{l+1} = x_l + f_l(x_l), Sec. III-A, for the
+ * rows of the verify block, or of single tokens).
+ *   x         bf16 [R, K] row-major
+ *   codes     uint8 [N, K / 2]: the rows of W (nn.Linear layout)
+ *   params    float16 [N, K / group, 2]: (scale, zero) of each group of K
+ *   residual  bf16 [R, N] added to the product, or NULL; may be `out` itself
+ *   out       bf16 [R, N] written
+ *   R, N, K, group   any R, N >= 1; group in {32, 64, 128}; K a multiple of group
+ *   status    device int32 (SPADE_DEV_TIMEOUT)
+ * Every pointer 16-byte aligned.  Products are summed in fp32 in an order that
+ * depends on the sizes alone.
+ */
+spade_status spade_linear_w4(const void *x, const void *codes, const void *params,
+                             const void *residual, void *out, int32_t R, int32_t N, int32_t K,
+                             int32_t group, int32_t *status, spade_stream_t stream);
+
+/*
+ * The verify block's query, key and value heads on their way into the attention:
+ * for row cu_q[b] + i at position pos = ctx_lens[b] + i
+ *   q_h, k_g: RMS norm of the head, y = x / sqrt(mean(x^2) + eps) * weight, where a
+ *     weight is given, then the rotation of the pairs (j, j + D/2) by the table's
+ *     angle: (a, b) -> (a cos - b sin, b cos + a sin);
+ *   q_out[cu_q[b] + i, h, :] = q_h rounded to bf16;
+ *   k_g and v_g (as they are) go into slot pos of the 4-bit cache, from fp32.
+ *   qkv       bf16 [R, (Hq + 2 Hkv) D]: a row's query heads, key heads, value heads
+ *   q_norm, k_norm   bf16 [D] norm weights, each or both NULL for no norm
+ *   rope      float32 [max_pos, D / 2, 2]: (cos, sin) of position and frequency j;
+ *             16-byte aligned
+ *   ctx_lens, n_draft, cu_q   as for the attention
+ *   max_k     bound of n_draft; eps  finite, >= 0
+ *   status    a sequence whose block is invalid, or whose positions pass max_pos
+ *             (SPADE_DEV_BAD_INDEX), or that does not fit its pages
+ *             (SPADE_DEV_CAPACITY) is skipped; a slot whose page is not in the pool
+ *             is not written (SPADE_DEV_BAD_INDEX)
+ * R has no upper limit: prompts are written by the same call.  B <= 65535.
+ */
+spade_status spade_verify_qk_norm_rope_kv4(
+    const void *qkv, const void *q_norm, const void *k_norm, const float *rope, void *q_out,
+    void *k_codes, void *k_params, void *v_codes, void *v_params, const int32_t *block_table,
+    const int32_t *ctx_lens, const int32_t *n_draft, const int32_t *cu_q, int32_t B, int32_t R,
+    int32_t Hq, int32_t Hkv, int32_t D, int32_t page_size, int32_t num_pages, int32_t max_pages,
+    int32_t max_pos, int32_t max_k, float eps, int32_t *status, spade_stream_t stream);
+
+/*
+ * spade_verify_attention_paged over the 4-bit cache: the same rows, mask, outputs,
+ * limits and workspace (spade_attn_workspace_size with cap = max_pages * page_size).
+ * A row sees slots [0, ctx_lens[b] + i] and nothing of any other, whatever those
+ * hold; a slot that it sees whose key or value has a scale that is not finite makes
+ * the row and its lse NaN.
+ * n_draft = 0 is decoding, one token per sequence.
+ */
+spade_status spade_verify_attention_kv4(
+    const void *q, const void *k_codes, const void *k_params, const void *v_codes,
+    const void *v_params, const int32_t *block_table, const int32_t *ctx_lens,
+    const int32_t *n_draft, const int32_t *cu_q, void *out, float *lse, int32_t B, int32_t Hq,
+    int32_t Hkv, int32_t D, int32_t page_size, int32_t num_pages, int32_t max_pages, int32_t max_k,
+    int32_t R, void *workspace, size_t workspace_bytes, int32_t *status, spade_stream_t stream);
+
+/*
+ * spade_kv_commit_paged on the 4-bit cache: the codes and params of the rejected
+ * slots [ctx_b + a_b + 1, ctx_b + n_draft[b]] become zero (the value 0) and
+ * new_ctx_lens[b] = ctx_lens[b] + a_b + 1.  new_ctx_lens may be ctx_lens itself
+ * (the update in place) or another array.  A sequence with an invalid block is left
+ * untouched and reported; its new_ctx_lens[b] is ctx_lens[b].
+ */
+spade_status spade_kv_commit_kv4(void *k_codes, void *k_params, void *v_codes, void *v_params,
+                                 const int32_t *block_table, const int32_t *ctx_lens,
+                                 const int32_t *accepted_len, const int32_t *n_draft,
+                                 int32_t *new_ctx_lens, int32_t B, int32_t Hkv, int32_t D,
+                                 int32_t page_size, int32_t num_pages, int32_t max_pages,
+                                 int32_t *status, spade_stream_t stream);
+
+/*
+ * The values that slots of the 4-bit cache hold, rounded to bf16 (to move a
+ * sequence into a bf16 cache, or to look at it): row cu_rows[b] + i of k_out and
+ * v_out is slot starts[b] + i of sequence b, 0 <= i < cu_rows[b + 1] - cu_rows[b].
+ *   starts    int32 [B];  cu_rows  int32 [B + 1], within [0, R]
+ *   k_out, v_out   bf16 [R, Hkv, D] written, 16-byte aligned
+ *   status    a sequence with bad offsets (SPADE_DEV_BAD_INDEX) or slots past its
+ *             capacity (SPADE_DEV_CAPACITY) is skipped; a page that is not in the
+ *             pool reads as zeros (SPADE_DEV_BAD_INDEX)
+ * B <= 65535.
+ */
+spade_status spade_kv_read_kv4(const void *k_codes, const void *k_params, const void *v_codes,
+                               const void *v_params, const int32_t *block_table,
+                               const int32_t *starts, const int32_t *cu_rows, void *k_out,
+                               void *v_out, int32_t B, int32_t R, int32_t Hkv, int32_t D,
+                               int32_t page_size, int32_t num_pages, int32_t max_pages,
+                               int32_t *status, spade_stream_t stream);
 
 /* ------------------------------------------------------------------------ */
 /* Diagnostics                                                               */

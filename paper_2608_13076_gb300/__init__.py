@@ -12,6 +12,12 @@ Entry points (same names as the C ABI in include/spade.h):
     spade_verify_accept     LM head + softmax + accept/reject + residual sampling
     spade_kv_commit         append accepted positions, roll back rejected ones
     spade_verify_qkv_rope   QKV projection + rotary embedding of the verify block, K/V into the cache
+and the verify step in 4 bits (weights and a paged cache; `int4` makes and reads their tensors):
+    spade_linear_w4                 projection with 4-bit weights (+ residual)
+    spade_verify_qk_norm_rope_kv4   head norms + rotary embedding, K/V into the 4-bit cache
+    spade_verify_attention_kv4      verify-position attention against the 4-bit cache
+    spade_kv_commit_kv4             the commit on the 4-bit cache
+    spade_kv_read_kv4               slots of the 4-bit cache as bf16 values
 """
 from __future__ import annotations
 
@@ -21,7 +27,7 @@ import os
 
 import torch
 
-from . import _build
+from . import _build, int4
 
 __all__ = [
     "SpadeError", "load", "build", "library_path",
@@ -32,6 +38,8 @@ __all__ = [
     "spade_accept_stats_layout", "read_accept_stats", "spade_verify_accept_commit",
     "spade_verify_accept_sampling", "spade_verify_accept_commit_paged", "spade_selftest_wait_timeout",
     "attn_workspace", "accept_workspace", "status_tensor", "check_status",
+    "spade_linear_w4", "spade_verify_qk_norm_rope_kv4", "spade_verify_attention_kv4", "spade_kv_commit_kv4",
+    "spade_kv_read_kv4", "int4",
     "DEV_BAD_INDEX", "DEV_CAPACITY", "DEV_TIMEOUT", "DEV_FALLBACK",
 ]
 
@@ -113,6 +121,16 @@ def load():
     lib.spade_verify_qkv_rope_paged.argtypes = [_vp] * 9 + [_i32] * 10 + [ctypes.c_float, _vp, _sz, _vp, _vp]
     lib.spade_kv_commit.restype = _i32
     lib.spade_kv_commit.argtypes = [_vp] * 5 + [_i32] * 4 + [_vp, _vp]
+    lib.spade_linear_w4.restype = _i32
+    lib.spade_linear_w4.argtypes = [_vp] * 5 + [_i32] * 4 + [_vp, _vp]
+    lib.spade_verify_qk_norm_rope_kv4.restype = _i32
+    lib.spade_verify_qk_norm_rope_kv4.argtypes = [_vp] * 13 + [_i32] * 10 + [ctypes.c_float, _vp, _vp]
+    lib.spade_verify_attention_kv4.restype = _i32
+    lib.spade_verify_attention_kv4.argtypes = [_vp] * 11 + [_i32] * 9 + [_vp, _sz, _vp, _vp]
+    lib.spade_kv_commit_kv4.restype = _i32
+    lib.spade_kv_commit_kv4.argtypes = [_vp] * 9 + [_i32] * 6 + [_vp, _vp]
+    lib.spade_kv_read_kv4.restype = _i32
+    lib.spade_kv_read_kv4.argtypes = [_vp] * 9 + [_i32] * 7 + [_vp, _vp]
     lib.spade_status_string.restype = ctypes.c_char_p
     lib.spade_status_string.argtypes = [_i32]
     lib.spade_last_error.restype = ctypes.c_char_p
@@ -376,3 +394,56 @@ def spade_kv_commit(k_cache, v_cache, ctx_lens, accepted_len, n_draft, *, status
     rc = (_native or native()).commit(k_cache, v_cache, ctx_lens, accepted_len, n_draft, status, stream)
     if rc:
         _check_rc(rc)
+
+
+# ---------------------------------------------------------------------------
+# The verify step in 4 bits (tensors of the formats in include/spade.h; see int4.py).
+def spade_linear_w4(x, codes, params, out, residual=None, *, status, stream=None):
+    """out = x W^T (+ residual) with W in 4 bits: codes [N, K / 2] uint8, params [N, K / group, 2] float16."""
+    rc = (_native or native()).linear_w4(x, codes, params, out, residual, status, stream)
+    if rc:
+        _check_rc(rc)
+    return out
+
+
+def spade_verify_qk_norm_rope_kv4(qkv, q_norm, k_norm, rope, q_out, k_codes, k_params, v_codes, v_params, block_table,
+                                  ctx_lens, n_draft, cu_q, *, eps, max_k, status, stream=None):
+    """Query and key heads of qkv [R, (Hq + 2 Hkv) D] normed (weights [D] or None) and turned by the table rope
+    [max_pos, D / 2, 2] at ctx + i; queries to q_out, keys and values into slots ctx .. ctx + k of the 4-bit cache."""
+    rc = (_native or native()).norm_rope_kv4(
+        qkv, q_norm, k_norm, rope, q_out, k_codes, k_params, v_codes, v_params, block_table, ctx_lens, n_draft, cu_q,
+        eps, max_k, status, stream)
+    if rc:
+        _check_rc(rc)
+    return q_out
+
+
+def spade_verify_attention_kv4(q, k_codes, k_params, v_codes, v_params, block_table, ctx_lens, n_draft, cu_q, out,
+                               lse=None, *, max_k, workspace, status, stream=None):
+    """spade_verify_attention_paged over the 4-bit cache (workspace: attn_workspace with cap = max_pages * page_size)."""
+    rc = (_native or native()).attention_kv4(
+        q, k_codes, k_params, v_codes, v_params, block_table, ctx_lens, n_draft, cu_q, out, lse, max_k, workspace,
+        status, stream)
+    if rc:
+        _check_rc(rc)
+    return out
+
+
+def spade_kv_commit_kv4(k_codes, k_params, v_codes, v_params, block_table, ctx_lens, accepted_len, n_draft,
+                        new_ctx_lens, *, status, stream=None):
+    """new_ctx_lens = ctx_lens + accepted_len + 1 (may be ctx_lens itself); rejected slots are cleared."""
+    rc = (_native or native()).commit_kv4(
+        k_codes, k_params, v_codes, v_params, block_table, ctx_lens, accepted_len, n_draft, new_ctx_lens, status, stream)
+    if rc:
+        _check_rc(rc)
+    return new_ctx_lens
+
+
+def spade_kv_read_kv4(k_codes, k_params, v_codes, v_params, block_table, starts, cu_rows, k_out, v_out, *, status,
+                      stream=None):
+    """Rows cu_rows[b] .. cu_rows[b + 1] of k_out, v_out: the values in slots starts[b] .. of sequence b."""
+    rc = (_native or native()).read_kv4(
+        k_codes, k_params, v_codes, v_params, block_table, starts, cu_rows, k_out, v_out, status, stream)
+    if rc:
+        _check_rc(rc)
+    return k_out, v_out

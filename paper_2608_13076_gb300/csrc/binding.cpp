@@ -25,6 +25,7 @@ const char *type_name(ScalarType t) {
     case ScalarType::BFloat16: return "torch.bfloat16";
     case ScalarType::Float: return "torch.float32";
     case ScalarType::Int: return "torch.int32";
+    case ScalarType::Half: return "torch.float16";
     default: return "torch.uint8";
   }
 }
@@ -408,11 +409,129 @@ PyObject *commit_paged(PyObject *, PyObject *const *a, Py_ssize_t n) {
   });
 }
 
+// ---- the verify step in 4 bits -----------------------------------------------------------------
+// The pools of a 4-bit cache and their table.
+struct Pools4 {
+  const at::Tensor &kc, &kp, &vc, &vp, &table;
+  int64_t num_pages, Hkv, page, D, max_pages, B;
+};
+// k_codes, k_params, v_codes, v_params, block_table
+Pools4 need_kv4(PyObject *const *a) {
+  const at::Tensor &kc = need(a[0], "k_codes", ScalarType::Byte, 4), &kp = need(a[1], "k_params", ScalarType::Half, 5);
+  const at::Tensor &vc = need(a[2], "v_codes", ScalarType::Byte, 4), &vp = need(a[3], "v_params", ScalarType::Half, 5);
+  const at::Tensor &t = need(a[4], "block_table", ScalarType::Int, 2);
+  const int64_t D = 2 * kc.size(3);
+  if (vc.sizes() != kc.sizes() || vp.sizes() != kp.sizes()) value_error("key and value pool shapes differ");
+  if (kp.size(0) != kc.size(0) || kp.size(1) != kc.size(1) || kp.size(2) != kc.size(2) || 64 * kp.size(3) != D ||
+      kp.size(4) != 2)
+    value_error("params must be [num_pages, Hkv, page_size, D / 64, 2] beside codes [num_pages, Hkv, page_size, D / 2]");
+  return Pools4{kc, kp, vc, vp, t, kc.size(0), kc.size(1), kc.size(2), D, t.size(1), t.size(0)};
+}
+
+// x, codes, params, out, residual, status, stream
+PyObject *linear_w4(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded(n, 7, [&] {
+    const at::Tensor &x = bf16(a[0], "x", 2), &codes = need(a[1], "codes", ScalarType::Byte, 2);
+    const at::Tensor &params = need(a[2], "params", ScalarType::Half, 3), &out = bf16(a[3], "out", 2);
+    const at::Tensor *res = a[4] == Py_None ? nullptr : &bf16(a[4], "residual", 2);
+    const at::Tensor &st = i32(a[5], "status");
+    const int64_t R = x.size(0), K = x.size(1), N = codes.size(0), groups = params.size(1);
+    if (2 * codes.size(1) != K || params.size(0) != N || params.size(2) != 2 || groups == 0 || K % groups ||
+        out.size(0) != R || out.size(1) != N || (res && res->sizes() != out.sizes()))
+      value_error("inconsistent linear_w4 shapes");
+    const spade_stream_t s = stream_of(a[6]);
+    const NoGil released;
+    return spade_linear_w4(x.data_ptr(), codes.data_ptr(), params.data_ptr(), res ? res->data_ptr() : nullptr,
+                           out.data_ptr(), n32(R), n32(N), n32(K), n32(K / groups), ip_mut(st), s);
+  });
+}
+
+// qkv, q_norm, k_norm, rope, q_out, pools (5), ctx_lens, n_draft, cu_q, eps, max_k, status, stream
+PyObject *norm_rope_kv4(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded(n, 17, [&] {
+    const at::Tensor &x = bf16(a[0], "qkv", 2), &rope = f32(a[3], "rope", 3), &q = bf16(a[4], "q_out", 3);
+    const at::Tensor *qn = a[1] == Py_None ? nullptr : &bf16(a[1], "q_norm", 1);
+    const at::Tensor *kn = a[2] == Py_None ? nullptr : &bf16(a[2], "k_norm", 1);
+    const Pools4 g = need_kv4(a + 5);
+    const at::Tensor &ctx = i32(a[10], "ctx_lens"), &nd = i32(a[11], "n_draft"), &cu = i32(a[12], "cu_q");
+    const at::Tensor &st = i32(a[15], "status");
+    const int64_t R = x.size(0), Hq = q.size(1);
+    if (q.size(0) != R || q.size(2) != g.D || x.size(1) != (Hq + 2 * g.Hkv) * g.D || rope.size(1) * 2 != g.D ||
+        rope.size(2) != 2 || (qn && qn->numel() != g.D) || (kn && kn->numel() != g.D) || ctx.numel() != g.B ||
+        nd.numel() != g.B || cu.numel() != g.B + 1)
+      value_error("inconsistent qk_norm_rope_kv4 shapes");
+    const spade_stream_t s = stream_of(a[16]);
+    const float eps = as_float(a[13]);
+    const int32_t max_k = as_int(a[14]);
+    const NoGil released;
+    return spade_verify_qk_norm_rope_kv4(
+        x.data_ptr(), qn ? qn->data_ptr() : nullptr, kn ? kn->data_ptr() : nullptr, fp(&rope), q.data_ptr(),
+        g.kc.data_ptr(), g.kp.data_ptr(), g.vc.data_ptr(), g.vp.data_ptr(), ip(g.table), ip(ctx), ip(nd), ip(cu),
+        n32(g.B), n32(R), n32(Hq), n32(g.Hkv), n32(g.D), n32(g.page), n32(g.num_pages), n32(g.max_pages),
+        n32(rope.size(0)), max_k, eps, ip_mut(st), s);
+  });
+}
+
+// q, pools (5), ctx_lens, n_draft, cu_q, out, lse, max_k, workspace, status, stream
+PyObject *attention_kv4(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded(n, 15, [&] {
+    const at::Tensor &q = bf16(a[0], "q", 3), &out = bf16(a[9], "out", 3);
+    const Pools4 g = need_kv4(a + 1);
+    const at::Tensor &ctx = i32(a[6], "ctx_lens"), &nd = i32(a[7], "n_draft"), &cu = i32(a[8], "cu_q");
+    const at::Tensor *lse = a[10] == Py_None ? nullptr : &f32(a[10], "lse", 2);
+    const at::Tensor &ws = u8(a[12], "workspace"), &st = i32(a[13], "status");
+    if (q.size(2) != g.D || out.sizes() != q.sizes() || ctx.numel() != g.B || nd.numel() != g.B ||
+        cu.numel() != g.B + 1 || (lse && (lse->size(0) != q.size(0) || lse->size(1) != q.size(1))))
+      value_error("inconsistent attention_kv4 shapes");
+    const spade_stream_t s = stream_of(a[14]);
+    const int32_t max_k = as_int(a[11]);
+    const NoGil released;
+    return spade_verify_attention_kv4(
+        q.data_ptr(), g.kc.data_ptr(), g.kp.data_ptr(), g.vc.data_ptr(), g.vp.data_ptr(), ip(g.table), ip(ctx), ip(nd),
+        ip(cu), out.data_ptr(), lse ? static_cast<float *>(lse->data_ptr()) : nullptr, n32(g.B), n32(q.size(1)),
+        n32(g.Hkv), n32(g.D), n32(g.page), n32(g.num_pages), n32(g.max_pages), max_k, n32(q.size(0)), ws.data_ptr(),
+        ws.numel(), ip_mut(st), s);
+  });
+}
+
+// pools (5), ctx_lens, accepted_len, n_draft, new_ctx_lens, status, stream
+PyObject *commit_kv4(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded(n, 11, [&] {
+    const Pools4 g = need_kv4(a);
+    const at::Tensor &ctx = i32(a[5], "ctx_lens"), &acc = i32(a[6], "accepted_len"), &nd = i32(a[7], "n_draft");
+    const at::Tensor &next = i32(a[8], "new_ctx_lens"), &st = i32(a[9], "status");
+    if (ctx.numel() != g.B || acc.numel() != g.B || nd.numel() != g.B || next.numel() != g.B)
+      value_error("inconsistent commit_kv4 shapes");
+    const spade_stream_t s = stream_of(a[10]);
+    const NoGil released;
+    return spade_kv_commit_kv4(g.kc.data_ptr(), g.kp.data_ptr(), g.vc.data_ptr(), g.vp.data_ptr(), ip(g.table), ip(ctx),
+                               ip(acc), ip(nd), ip_mut(next), n32(g.B), n32(g.Hkv), n32(g.D), n32(g.page),
+                               n32(g.num_pages), n32(g.max_pages), ip_mut(st), s);
+  });
+}
+
+// pools (5), starts, cu_rows, k_out, v_out, status, stream
+PyObject *read_kv4(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded(n, 11, [&] {
+    const Pools4 g = need_kv4(a);
+    const at::Tensor &starts = i32(a[5], "starts"), &cu = i32(a[6], "cu_rows"), &st = i32(a[9], "status");
+    const at::Tensor &k = bf16(a[7], "k_out", 3), &v = bf16(a[8], "v_out", 3);
+    if (starts.numel() != g.B || cu.numel() != g.B + 1 || k.size(1) != g.Hkv || k.size(2) != g.D || v.sizes() != k.sizes())
+      value_error("inconsistent read_kv4 shapes");
+    const spade_stream_t s = stream_of(a[10]);
+    const NoGil released;
+    return spade_kv_read_kv4(g.kc.data_ptr(), g.kp.data_ptr(), g.vc.data_ptr(), g.vp.data_ptr(), ip(g.table),
+                             ip(starts), ip(cu), k.data_ptr(), v.data_ptr(), n32(g.B), n32(k.size(0)), n32(g.Hkv),
+                             n32(g.D), n32(g.page), n32(g.num_pages), n32(g.max_pages), ip_mut(st), s);
+  });
+}
+
 #define ENTRY(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
     ENTRY(attention), ENTRY(attention_noalloc), ENTRY(attention_paged), ENTRY(accept), ENTRY(accept_commit),
     ENTRY(accept_sampling), ENTRY(accept_commit_paged), ENTRY(qkv), ENTRY(qkv_paged), ENTRY(commit),
-    ENTRY(commit_paged), {nullptr, nullptr, 0, nullptr}};
+    ENTRY(commit_paged), ENTRY(linear_w4), ENTRY(norm_rope_kv4), ENTRY(attention_kv4), ENTRY(commit_kv4),
+    ENTRY(read_kv4), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_spade_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

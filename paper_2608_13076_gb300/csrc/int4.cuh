@@ -1,0 +1,44 @@
+// int4.cuh -- numbers in 4 bits as include/spade.h lays them out: value = scale *
+// (code - zero), eight codes to a 32-bit word whose fields 4p .. 4p + 3 hold numbers
+// 0, 2, 4, 6, 1, 3, 5, 7, and (scale, zero) pairs of float16 per group.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include <cstdint>
+
+#include "ptx.cuh"
+
+namespace spade {
+namespace int4 {
+
+constexpr int kKvGroup = 64;          // dims of a head per (scale, zero) pair of the cache
+constexpr float kMaxScale = 4364.f;   // 15 steps of it stay within float16
+
+// Number i (compile-time after unrolling) of a word.
+SPADE_DEVICE uint32_t code_of(uint32_t w, int i) { return (w >> (4 * ((i >> 1) + 4 * (i & 1)))) & 15u; }
+
+// A 4-byte (scale, zero) pair as floats.
+SPADE_DEVICE float2 pair_of(uint32_t bits) {
+  const __half2 h = *reinterpret_cast<const __half2 *>(&bits);
+  return __half22float2(h);
+}
+
+// The cache's pages (see include/spade.h).
+struct Cache {
+  uint8_t *k_codes, *v_codes;
+  uint32_t *k_params, *v_params;  // one (scale, zero) pair per entry
+  const int32_t *block_table;
+  int Hkv, D, page_size, num_pages, max_pages;
+  __device__ int64_t capacity() const { return static_cast<int64_t>(max_pages) * page_size; }
+  // Pool row of head 0 of sequence b's slot, in rows of D / 2 code bytes (head h is
+  // h * page_size rows on); negative where the page is not in the pool.
+  __device__ int64_t row(int b, int slot) const {
+    const int page = __ldg(block_table + static_cast<int64_t>(b) * max_pages + slot / page_size);
+    if (page < 0 || page >= num_pages) return -1;
+    return static_cast<int64_t>(page) * Hkv * page_size + slot % page_size;
+  }
+};
+
+}  // namespace int4
+}  // namespace spade

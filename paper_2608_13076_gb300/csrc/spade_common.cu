@@ -66,8 +66,8 @@ EncodeFn g_encode = nullptr;
 std::once_flag g_encode_once;
 }  // namespace
 
-bool encode_tmap_bf16_sw128_nd(CUtensorMap *map, const void *base, uint32_t rank, const uint64_t *dims,
-                               const uint64_t *strides_bytes, const uint32_t *box) {
+static bool encode_tmap(CUtensorMap *map, CUtensorMapDataType type, CUtensorMapSwizzle swizzle, const void *base,
+                        uint32_t rank, const uint64_t *dims, const uint64_t *strides_bytes, const uint32_t *box) {
   std::call_once(g_encode_once, [] {
     void *fn = nullptr;
     cudaDriverEntryPointQueryResult q;
@@ -88,8 +88,8 @@ bool encode_tmap_bf16_sw128_nd(CUtensorMap *map, const void *base, uint32_t rank
     es[i] = 1;
     if (i + 1 < rank) s[i] = strides_bytes[i];
   }
-  const CUresult r = g_encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void *>(base), d, s, b, es,
-                              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+  const CUresult r = g_encode(map, type, rank, const_cast<void *>(base), d, s, b, es,
+                              CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
                               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) {
     fail(SPADE_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d): %u-D, inner %llu, rows %llu, box %u x %u",
@@ -97,6 +97,26 @@ bool encode_tmap_bf16_sw128_nd(CUtensorMap *map, const void *base, uint32_t rank
     return false;
   }
   return true;
+}
+
+bool encode_tmap_bf16_sw128_nd(CUtensorMap *map, const void *base, uint32_t rank, const uint64_t *dims,
+                               const uint64_t *strides_bytes, const uint32_t *box) {
+  return encode_tmap(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, CU_TENSOR_MAP_SWIZZLE_128B, base, rank, dims, strides_bytes,
+                     box);
+}
+
+bool encode_tmap_bytes(CUtensorMap *map, const void *base, uint32_t row_bytes, uint64_t rows, uint32_t box_rows) {
+  const uint64_t dims[2] = {row_bytes, rows}, strides[1] = {row_bytes};
+  const uint32_t box[2] = {row_bytes, box_rows};
+  return encode_tmap(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, row_bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B
+                                                                        : CU_TENSOR_MAP_SWIZZLE_32B,
+                     base, 2, dims, strides, box);
+}
+
+bool encode_tmap_words(CUtensorMap *map, const void *base, uint32_t row_words, uint64_t rows) {
+  const uint64_t dims[2] = {row_words, rows}, strides[1] = {static_cast<uint64_t>(row_words) * 4};
+  const uint32_t box[2] = {row_words, 1};
+  return encode_tmap(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, CU_TENSOR_MAP_SWIZZLE_NONE, base, 2, dims, strides, box);
 }
 
 bool encode_tmap_bf16_sw128(CUtensorMap *map, const void *base, uint64_t inner, uint64_t rows,

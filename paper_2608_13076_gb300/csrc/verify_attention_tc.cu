@@ -82,107 +82,6 @@ static_assert(Smem::RMAX % 16 == 0, "row maxima are read as float4");
 static_assert(Smem::BYTES <= 225 * 1024, "shared memory budget");
 static_assert(Smem::Q % 1024 == 0 && Smem::P % 1024 == 0, "swizzled tiles need 1024-byte alignment");
 
-// Shared-memory descriptor of a 128-byte-swizzled operand.  K-major: 8-row
-// groups `sbo` apart (lbo unused).  MN-major: 64-element blocks along M/N are
-// `lbo` apart and 8-row groups along K are `sbo` apart.
-__device__ __forceinline__ uint64_t desc_sw128(uint32_t saddr, uint32_t lbo, uint32_t sbo) {
-  uint64_t d = 0;
-  d |= static_cast<uint64_t>((saddr & 0x3FFFF) >> 4);
-  d |= static_cast<uint64_t>((lbo >> 4) & 0x3FFF) << 16;
-  d |= static_cast<uint64_t>((sbo >> 4) & 0x3FFF) << 32;
-  d |= static_cast<uint64_t>(1) << 46;  // descriptor version (sm_100 family)
-  d |= static_cast<uint64_t>(2) << 61;  // 128-byte swizzle
-  return d;
-}
-
-// barrier.red.or over `threads` threads of named barrier `id`.
-__device__ __forceinline__ bool bar_any(int id, int threads, bool pred) {
-  uint32_t r;
-  __syncwarp();
-  asm volatile(
-      "{\n\t.reg .pred p, q;\n\t"
-      "setp.ne.u32 p, %1, 0;\n\t"
-      "barrier.red.or.pred q, %2, %3, p;\n\t"
-      "selp.u32 %0, 1, 0, q;\n\t}"
-      : "=r"(r)
-      : "r"(static_cast<uint32_t>(pred)), "r"(id), "r"(threads)
-      : "memory");
-  return r != 0;
-}
-
-// Reduce-scatter over the warp of NP values per lane (NP a power of two,
-// <= 32): on return lane L holds the reduction over all 32 lanes of value
-// L % NP.  Each step halves the values a lane keeps (it sends the half its
-// partner keeps), so NP - 1 + log2(32 / NP) shuffles in all.  `v` is consumed.
-template <int NP, bool kMax>
-__device__ __forceinline__ float warp_reduce_scatter(float (&v)[NP], int lane) {
-#pragma unroll
-  for (int h = NP / 2; h >= 1; h /= 2) {
-    const bool upper = (lane & h) != 0;
-#pragma unroll
-    for (int i = 0; i < h; ++i) {
-      const float send = upper ? v[i] : v[i + h];
-      const float keep = upper ? v[i + h] : v[i];
-      const float got = __shfl_xor_sync(0xffffffffu, send, h);
-      v[i] = kMax ? fmaxf(keep, got) : keep + got;
-    }
-  }
-  float r = v[0];
-#pragma unroll
-  for (int o = NP; o < 32; o *= 2) {
-    const float got = __shfl_xor_sync(0xffffffffu, r, o);
-    r = kMax ? fmaxf(r, got) : r + got;
-  }
-  return r;
-}
-
-// 16-byte global -> shared copy (cp.async); src_bytes = 0 writes zeros.
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, uint32_t src_bytes) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(src_bytes)
-               : "memory");
-}
-__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void cp_async_wait() {
-  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
-}
-
-// One segment of a CTA's range: the part of one unit's cost span in
-// [x, seg_end); its real key slices are g.ci .. g.ci + n_here - 1.
-struct SegInfo {
-  Seg g;
-  int64_t seg_end;
-  int n_here;   // key slices in this segment (0: only the unit's virtual start)
-  int nchunk;   // MMA chunks (pairs of slices, the last one possibly single)
-};
-__device__ __forceinline__ SegInfo seg_of(const Sched &sc, const Seg &g, int64_t x, int64_t x_end) {
-  SegInfo s;
-  s.g = g;
-  s.seg_end = min(x_end, s.g.ust + sc.E + s.g.nch);
-  const int lo = max(0, static_cast<int>(x - s.g.ust) - sc.E);
-  const int hi = max(0, static_cast<int>(s.seg_end - s.g.ust) - sc.E);
-  s.g.ci = lo;
-  s.n_here = hi - lo;
-  s.nchunk = (s.n_here + 1) / 2;
-  return s;
-}
-__device__ __forceinline__ SegInfo seg_at(const Sched &sc, int64_t x, int64_t x_end) {
-  return seg_of(sc, locate(sc, x), x, x_end);
-}
-// The first segment at or after cost position x that holds key slices (all
-// roles skip the same empty ones); n_here == 0 when the range has none left.
-__device__ __forceinline__ SegInfo next_seg(const Sched &sc, int64_t x, int64_t x_end) {
-  SegInfo s = seg_at(sc, x, x_end);
-  while (s.n_here == 0 && s.seg_end < x_end) s = seg_at(sc, s.seg_end, x_end);
-  return s;
-}
-// The same, computed by a whole warp (every lane gets the result).
-__device__ __forceinline__ SegInfo next_seg_warp(const Sched &sc, int64_t x, int64_t x_end, int lane) {
-  SegInfo s = seg_of(sc, locate_warp(sc, x, lane), x, x_end);
-  while (s.n_here == 0 && s.seg_end < x_end) s = seg_of(sc, locate_warp(sc, s.seg_end, lane), s.seg_end, x_end);
-  return s;
-}
-
 // D: head dim, 64 or 128.  With D = 64 the K and V tiles hold one 64-dim slab
 // and the V tiles' second slab stays zero, so O^T keeps M = 128 (its rows
 // 64-127 are zero and never stored).

@@ -20,7 +20,7 @@ constexpr int kChunk = 64;     // keys per schedule slice (two per MMA chunk)
 constexpr int kRowBlock = 64;  // query rows per work unit
 constexpr int kMaxB = 512;     // sequences per call (per-CTA schedule lives in smem)
 constexpr int kUnitCostTc = 11; // virtual slices per unit in the tensor-memory kernel's schedule
-constexpr int kUnitCostKv4 = 24; // the same for the 4-bit cache, whose slices are shorter
+constexpr int kUnitCostKv4 = 10; // the same for the 4-bit cache, whose slices are shorter
 
 struct Params {
   const __nv_bfloat16 *q;

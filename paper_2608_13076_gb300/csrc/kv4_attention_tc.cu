@@ -65,9 +65,14 @@ constexpr int kFirst = 1, kLast = 2, kEnd = 4;
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kColS = 0, kColO = 256, kColK = 320;
 
-constexpr int kBarFull = 0, kBarEmpty = 4, kBarKFull = 8, kBarKFree = 10, kBarSFull = 12, kBarSFree = 14,
-              kBarVFull = 16, kBarVFree = 18, kBarPFull = 20, kBarPFree = 22, kBarScale = 24, kBarODone = 28,
-              kBarSeg = 29, kBarOFinal = 30, kBarQ = 31, kBarDrain = 32, kNumBars = 33;
+// mbarriers.  The MMA warp issues S(j), PV(j-1), S(j+1), ... and a commit completes when
+// every MMA before it has, so two commits per chunk say everything: SDone (S(j)) that
+// the keys' columns of chunk j and, through PV(j-2) before it, the weights' buffer of
+// chunk j-2 are free; PVDone (PV(j)) that the values' buffer is, and O^T complete.  The
+// scores' buffer is free once the weights are written, which PV(j-2) waited for.  No
+// phase can run two ahead of a waiter: each next one needs the waiter's own next arrival.
+constexpr int kBarFull = 0, kBarEmpty = 4, kBarKFull = 8, kBarSDone = 10, kBarVFull = 12, kBarPVDone = 14,
+              kBarPFull = 16, kBarScale = 18, kBarSeg = 22, kBarQ = 23, kBarDrain = 24, kNumBars = 25;
 
 struct Smem {
   static constexpr int RING = 0;
@@ -82,7 +87,7 @@ struct Smem {
   static constexpr int KD = CTX + kMaxB * 4;
   static constexpr int WRED = round_up_c(KD + kMaxB * 4, 128);
   static constexpr int ROWV = WRED + 4 * kRowBlock * 4;
-  static constexpr int RMAX = ROWV + kRowBlock * 4;         // float [64 rows]: running maximum - kPBias
+  static constexpr int RMAX = ROWV + kRowBlock * 4;         // float [64 rows]: kPBias - running maximum
   static constexpr int ALPHA = RMAX + kRowBlock * 4;
   static constexpr int BAR = ALPHA + kRowBlock * 4;
   static constexpr int MISC = BAR + kNumBars * 8;           // abort, last, tmem base
@@ -100,7 +105,7 @@ static_assert(Smem::BYTES <= 227 * 1024, "shared memory budget");
 SPADE_DEVICE void unpack_bf16(uint32_t w, __nv_bfloat162 nz, uint32_t *out) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    const uint32_t u = ((w >> (4 * e)) & 0x000f000fu) | 0x43004300u;
+    const uint32_t u = and_or(w >> (4 * e), 0x000f000fu, 0x43004300u);
     const __nv_bfloat162 v = __hadd2(*reinterpret_cast<const __nv_bfloat162 *>(&u), nz);
     out[e] = *reinterpret_cast<const uint32_t *>(&v);
   }
@@ -111,7 +116,7 @@ SPADE_DEVICE void unpack_fp16(uint32_t w, __half2 s, __half2 nz, __half2 nz16, u
   const __half2 sixteenth = __float2half2_rn(0.0625f);
 #pragma unroll
   for (int e = 0; e < 2; ++e) {
-    const uint32_t lo = (w & 0x000f000fu) | 0x64006400u, hi = (w & 0x00f000f0u) | 0x64006400u;
+    const uint32_t lo = and_or(w, 0x000f000fu, 0x64006400u), hi = and_or(w, 0x00f000f0u, 0x64006400u);
     const __half2 a = __hmul2(__hadd2(*reinterpret_cast<const __half2 *>(&lo), nz), s);
     const __half2 b = __hmul2(__hfma2(*reinterpret_cast<const __half2 *>(&hi), sixteenth, nz16), s);
     out[2 * e] = *reinterpret_cast<const uint32_t *>(&a);
@@ -183,19 +188,14 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       for (int s = 0; s < kStages; ++s) {
         mbar_init(&bars[kBarKFull + s], 4);
-        mbar_init(&bars[kBarKFree + s], 1);
-        mbar_init(&bars[kBarSFull + s], 1);
-        mbar_init(&bars[kBarSFree + s], kSoftWarps);
+        mbar_init(&bars[kBarSDone + s], 1);
         mbar_init(&bars[kBarVFull + s], 4);
-        mbar_init(&bars[kBarVFree + s], 1);
+        mbar_init(&bars[kBarPVDone + s], 1);
         mbar_init(&bars[kBarPFull + s], kSoftWarps);
-        mbar_init(&bars[kBarPFree + s], 1);
       }
       for (int s = 0; s < kScaleSlots; ++s) mbar_init(&bars[kBarScale + s], 4);
-      mbar_init(&bars[kBarODone], 1);
       mbar_init(&bars[kBarSeg], kSoftWarps);
       mbar_init(&bars[kBarQ], kSoftWarps);
-      mbar_init(&bars[kBarOFinal], 1);
       mbar_init(&bars[kBarDrain], 1);
       fence_mbar_init();
     }
@@ -315,39 +315,37 @@ __global__ void __launch_bounds__(kThreads, 1)
     const bool leader = elect_one();
     bool ok = true;
     uint32_t it = 0, seg = 0;
-    auto issue_pv = [&](uint32_t j, bool first, bool last) {
+    // (The flag is looked at once per chunk.)
+    auto wait = [&](int bar, uint32_t parity) {
+      ok = __all_sync(0xffffffffu, mbar_wait_lean(&bars[bar], parity, s_abort)) && ok;
+    };
+    auto issue_pv = [&](uint32_t j, bool first) {
       const int st = j % kStages;
       const uint32_t ph = (j / kStages) & 1;
-      ok &= warp_wait(&bars[kBarVFull + st], ph, s_abort);
-      ok &= warp_wait(&bars[kBarPFull + st], ph, s_abort);
+      wait(kBarVFull + st, ph);
+      wait(kBarPFull + st, ph);
       // The segment's first PV overwrites O^T: the previous epilogue has read it.
-      if (first) ok &= warp_wait(&bars[kBarSeg], seg & 1, s_abort);
+      if (first) wait(kBarSeg, seg & 1);
       tc_fence_after();
       const uint64_t dv = desc_sw128(smem_base + Smem::V + st * kTile, kSlab, 1024);
       const uint64_t dp = desc_sw128(smem_base + Smem::P + st * kPBytes, kSlab, 1024);
 #pragma unroll
       for (int kk = 0; kk < kKeys / 16; ++kk)
         if (leader) tc_mma_f16(tmem + kColO, dv + 128u * kk, dp + 128u * kk, idesc_pv, (first && kk == 0) ? 0u : 1u);
-      if (leader) {
-        tc_commit(&bars[kBarVFree + st]);
-        tc_commit(&bars[kBarPFree + st]);
-        tc_commit(&bars[kBarODone]);
-        if (last) tc_commit(&bars[kBarOFinal]);
-      }
+      if (leader) tc_commit(&bars[kBarPVDone + st]);
     };
     bool before_first = false;  // whether the chunk before was the first of its segment
-    while (true) {
+    while (!__any_sync(0xffffffffu, *s_abort != 0)) {
       const int st = it % kStages;
       const uint32_t ph = (it / kStages) & 1;
-      ok &= warp_wait(&bars[kBarKFull + st], ph, s_abort);
+      wait(kBarKFull + st, ph);
       if (!ok) break;
       const int flags = uniform(s_cmeta[it % kScaleSlots]);
       if (flags & kEnd) break;
       const bool first = flags & kFirst;
       // The segment's Q is staged: its S products may start while the previous
       // segment's epilogue still reads O^T.
-      if (first) ok &= warp_wait(&bars[kBarQ], seg & 1, s_abort);
-      ok &= warp_wait(&bars[kBarSFree + st], ph ^ 1, s_abort);
+      if (first) wait(kBarQ, seg & 1);
       tc_fence_after();
       const uint64_t dq = desc_sw128(smem_base + Smem::Q + (seg & 1) * 2 * kQSlab, 16, 1024);
 #pragma unroll
@@ -360,21 +358,18 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (leader) tc_mma_f16_ta(d, a, dq + qo, idesc_s, kk > 0 ? 1u : 0u);
         }
       }
-      if (leader) {
-        tc_commit(&bars[kBarSFull + st]);
-        tc_commit(&bars[kBarKFree + st]);
-      }
-      if (!first) issue_pv(it - 1, before_first, false);
+      if (leader) tc_commit(&bars[kBarSDone + st]);
+      if (!first) issue_pv(it - 1, before_first);
       if (!ok) break;
       if (flags & kLast) {
-        issue_pv(it, first, true);
+        issue_pv(it, first);
         if (!ok) break;
         ++seg;
       }
       before_first = first;
       ++it;
     }
-    if (!ok && leader) {
+    if (leader && (!ok || *s_abort)) {
       atomicOr(p.status, SPADE_DEV_TIMEOUT);
       tc_commit(&bars[kBarDrain]);
       mbar_wait_unabortable(&bars[kBarDrain], 0);
@@ -390,9 +385,12 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int rs = it % kRing, st = it % kStages;
       const uint32_t ph = (it / kStages) & 1;
       const uint8_t *stage = smem + Smem::RING + rs * kStage;
-      ok = warp_wait(&bars[kBarFull + rs], (it / kRing) & 1, s_abort) &&
-           warp_wait(&bars[(is_v ? kBarVFree : kBarKFree) + st], ph ^ 1, s_abort);
-      if (!ok) break;
+      ok = *s_abort == 0 && mbar_wait_lean(&bars[kBarFull + rs], (it / kRing) & 1, s_abort) &&
+           mbar_wait_lean(&bars[(is_v ? kBarPVDone : kBarSDone) + st], ph ^ 1, s_abort);
+      if (!__all_sync(0xffffffffu, ok)) {
+        ok = false;
+        break;
+      }
       const int2 meta = s_rmeta[rs];
       if (!is_v && warp == kWarpK && lane == 0) s_cmeta[it % kScaleSlots] = meta.y;
       if (meta.y & kEnd) {
@@ -501,7 +499,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int nrow = min(kRowBlock, p.G * (kd + 1) - kRowBlock * g.rb);
       const int q_row0 = p.cu_q[g.b];
       const int hi = nrow - c0;            // rows r < hi of this warp are real
-      if (stid < kRowBlock) s_rmax[stid] = -INFINITY;
+      // Rows past nrow (zeros in Q, never stored) keep a maximum of 0, so that only keys
+      // need masks.
+      if (stid < kRowBlock) s_rmax[stid] = stid < nrow ? INFINITY : 0.f;
       cp_async_wait<0>();  // this segment's Q has landed
       fence_proxy_async_smem();
       named_bar(1, kSoftThreads);
@@ -518,11 +518,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       cp_async_commit();
 
-      float l[NH], x_[NP];
+      float x_[NP];
+      F2 l2[NH / 2];  // row sums of this key lane, rows in pairs
 #pragma unroll
-      for (int r = 0; r < NH; ++r) l[r] = 0.f;
-      const float4 *rmax4 = reinterpret_cast<const float4 *>(s_rmax + c0);
-
+      for (int r = 0; r < NH / 2; ++r) l2[r] = f2(0.f, 0.f);
       for (int c = 0; c < si.nchunk; ++c, ++it) {
         const int st = it % kStages;
         const uint32_t ph = (it / kStages) & 1;
@@ -530,59 +529,61 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int nk = min(2, si.n_here - 2 * c) * kChunk;
         const int kg = key0 + t;
         // Row R = 64 rb + rr (position R / G) sees key kg iff R >= (kg - ctx) G.
-        const int lo = (t < nk) ? max(0, (kg - ctx) * p.G - kRowBlock * g.rb) - c0 : NH;
+        const int lo = (t < nk) ? (kg - ctx) * p.G - kRowBlock * g.rb - c0 : NH;
+        const bool masked = __any_sync(0xffffffffu, lo > 0);  // (the last keys of a sequence or segment)
         const uint32_t taddr = tlane + kColS + st * NG * 64 + c0;
 
-        // Scores of this key lane, in log2 units: the groups' sums under their scales.
-        if (!mbar_wait(&bars[kBarScale + it % kScaleSlots], (it / kScaleSlots) & 1, s_abort)) expired = true;
+        // Scores of this key lane relative to `off` (one per row), in log2 units: the groups'
+        // sums under their scales.
+        expired = expired || *s_abort || !mbar_wait_lean(&bars[kBarScale + it % kScaleSlots], (it / kScaleSlots) & 1, s_abort);
         const float2 sk = s_scale[(it % kScaleSlots) * kKeys + t];
-        auto load_scores = [&]() {
+        auto load_scores = [&](const float *off) {
 #pragma unroll
-          for (int j = 0; j < NH / 8; ++j) tmem_ld8(taddr + j * 8, reinterpret_cast<uint32_t *>(x_) + j * 8);
-          if constexpr (NG == 2) {
+          for (int r0 = 0; r0 < NH; r0 += 16) {  // 16 rows at a time: registers
+            constexpr int kMost = NH < 16 ? NH : 16;
+            uint32_t y[NG][kMost];
 #pragma unroll
-            for (int j = 0; j < NH / 8; ++j) {
-              uint32_t y[8];
-              tmem_ld8(taddr + 64 + j * 8, y);
-              tmem_wait_ld();
+            for (int g2 = 0; g2 < NG; ++g2)
 #pragma unroll
-              for (int e = 0; e < 8; ++e)
-                x_[j * 8 + e] = fmaf(__uint_as_float(y[e]), sk.y, x_[j * 8 + e] * sk.x);
-            }
-          } else {
+              for (int j = 0; j < kMost && r0 + j < NH; j += 8) tmem_ld8(taddr + g2 * 64 + r0 + j, y[g2] + j);
             tmem_wait_ld();
 #pragma unroll
-            for (int r = 0; r < NH; ++r) x_[r] *= sk.x;
+            for (int j = 0; j < kMost && r0 + j < NH; j += 4) {
+              const float4 mv = off ? *reinterpret_cast<const float4 *>(off + r0 + j)
+                                    : make_float4(-kPBias, -kPBias, -kPBias, -kPBias);
+#pragma unroll
+              for (int e = 0; e < 4; e += 2) {
+                // -m = inf (no visible key yet) gives inf for a visible score: a vote.
+                // (The score is rounded before the maximum is taken off, as where it was found:
+                // the largest one's weight is 2^kPBias whatever the scores' size.)
+                F2 s = f2_mul(f2(__uint_as_float(y[0][j + e]), __uint_as_float(y[0][j + e + 1])), f2(sk.x, sk.x));
+                if constexpr (NG == 2)
+                  s = f2_fma(f2(__uint_as_float(y[NG - 1][j + e]), __uint_as_float(y[NG - 1][j + e + 1])),
+                             f2(sk.y, sk.y), s);
+                s = f2_add(s, e ? f2(mv.z, mv.w) : f2(mv.x, mv.y));
+                f2_split(s, x_[r0 + j + e], x_[r0 + j + e + 1]);
+              }
+            }
+          }
+          if (masked) {
+#pragma unroll
+            for (int r = 0; r < NH; ++r) x_[r] = r < lo ? -INFINITY : x_[r];
           }
         };
-        if (!mbar_wait(&bars[kBarSFull + st], ph, s_abort)) expired = true;
-        tc_fence_after();
-        load_scores();
-        tc_fence_before();
+        expired = expired || !mbar_wait_lean(&bars[kBarSDone + st], ph, s_abort);
         __syncwarp();
-        if (lane == 0) mbar_arrive(&bars[kBarSFree + st]);
-        bool exceed = false;
+        tc_fence_after();
+        load_scores(s_rmax + c0);
+        float high = fmaxf(x_[0], x_[1]);
 #pragma unroll
-        for (int r4 = 0; r4 < NH / 4; ++r4) {
-          const float4 mv = rmax4[r4];
-          const float mm[4] = {mv.x, mv.y, mv.z, mv.w};
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int r = r4 * 4 + e;
-            const bool vis = r >= lo && r < hi;
-            // m = -inf (no visible key yet) gives +inf for a visible score: a vote.
-            x_[r] = vis ? x_[r] - mm[e] : -INFINITY;
-            exceed |= x_[r] > kRescaleLog2;
-          }
-        }
+        for (int r = 2; r < NH; r += 2) high = max3(high, x_[r], x_[r + 1]);
         // The two halves own disjoint rows: each votes and rescales on its own barriers.
-        if (bar_any(2 + half, kSoftThreads / 2, exceed)) {
+        if (bar_any(2 + half, kSoftThreads / 2, high > kRescaleLog2)) {
           // Some weight would pass 2^15 (always so in a unit's first chunk): take this
           // chunk's exact row maxima.  (S^T is reused only after this chunk's P is signalled.)
-          load_scores();
+          load_scores(nullptr);
 #pragma unroll
-          for (int r = 0; r < NP; ++r)
-            x_[r] = (r < NH && r >= lo && r < hi) ? x_[r] - kPBias : -INFINITY;
+          for (int r = NH; r < NP; ++r) x_[r] = -INFINITY;
           {
             const float wm = warp_reduce_scatter<NP, true>(x_, lane);
             if (lane < NH) s_wred[q4 * kRowBlock + c0 + lane] = wm;
@@ -591,19 +592,18 @@ __global__ void __launch_bounds__(kThreads, 1)
           const int hs = stid - half * (kSoftThreads / 2);
           if (hs < NH) {
             const int row = c0 + hs;
-            const float mo = s_rmax[row];
+            const float mo = -s_rmax[row];
             const float mn = fmaxf(fmaxf(mo, fmaxf(s_wred[row], s_wred[kRowBlock + row])),
                                    fmaxf(s_wred[2 * kRowBlock + row], s_wred[3 * kRowBlock + row]));
             s_alpha[row] = mn > mo ? ex2(mo - mn) : 1.f;  // mo = -inf gives 0: nothing to keep
-            s_rmax[row] = mn;
+            s_rmax[row] = -mn;
           }
           named_bar(4 + half, kSoftThreads / 2);
 #pragma unroll
-          for (int r = 0; r < NH; ++r) l[r] *= s_alpha[c0 + r];
+          for (int r = 0; r < NH / 2; ++r) l2[r] = f2_mul(l2[r], f2(s_alpha[c0 + 2 * r], s_alpha[c0 + 2 * r + 1]));
           if (c > 0) {
-            // O^T's columns are rescaled once the last PV has landed (S of this chunk has
-            // completed, so ODone is at most one phase behind).
-            if (!mbar_wait(&bars[kBarODone], (it - 1) & 1, s_abort)) expired = true;
+            // O^T's columns are rescaled once the last PV has landed.
+            if (!mbar_wait(&bars[kBarPVDone + (it - 1) % kStages], ((it - 1) / kStages) & 1, s_abort)) expired = true;
             tc_fence_after();
 #pragma unroll
             for (int j = 0; j < NH / 8; ++j) {
@@ -617,13 +617,10 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             tmem_wait_st();
           }
-          load_scores();
-#pragma unroll
-          for (int r = 0; r < NH; ++r) x_[r] = (r >= lo && r < hi) ? x_[r] - s_rmax[c0 + r] : -INFINITY;
+          load_scores(s_rmax + c0);
         }
 
         // ---- P^T row of this key (this warp's rows): fp16, 128-byte swizzle ----
-        if (!mbar_wait(&bars[kBarPFree + st], ph ^ 1, s_abort)) expired = true;
         uint8_t *prow = smem + Smem::P + st * kPBytes + t * 128;
 #pragma unroll
         for (int j = 0; j < NH / 8; ++j) {
@@ -632,8 +629,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           for (int e = 0; e < 4; ++e) {
             const int r0 = j * 8 + 2 * e;
             const float p0 = ex2(x_[r0]), p1 = ex2(x_[r0 + 1]);
-            l[r0] += p0;
-            l[r0 + 1] += p1;
+            l2[r0 / 2] = f2_add(l2[r0 / 2], f2(p0, p1));
             const __half2 h = __floats2half2_rn(p0, p1);
             w[e] = *reinterpret_cast<const uint32_t *>(&h);
           }
@@ -655,11 +651,15 @@ __global__ void __launch_bounds__(kThreads, 1)
 
       // ---- epilogue: row sums, O^T from tensor memory, output or partial ----
       const bool row_writer = q4 == 0 && lane < NH && lane < hi;
-      const float m_own = row_writer ? s_rmax[c0 + lane] : 0.f;
+      const float m_own = row_writer ? -s_rmax[c0 + lane] : 0.f;
+      float l[NH];
       {
         float v[NP];
 #pragma unroll
-        for (int r = 0; r < NP; ++r) v[r] = r < NH ? l[r] : 0.f;
+        for (int r = 0; r < NP; r += 2) {
+          v[r] = v[r + 1] = 0.f;
+          if (r < NH) f2_split(l2[r / 2], v[r], v[r + 1]);
+        }
         const float ws = warp_reduce_scatter<NP, false>(v, lane);
         if (lane < NH) s_wred[q4 * kRowBlock + c0 + lane] = ws;
       }
@@ -675,7 +675,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int64_t c_first = sc.owner(g.ust + sc.E);
       const int64_t c_last = sc.owner(g.ust + sc.E + g.nch - 1);
       const int nparts = static_cast<int>(c_last - c_first + 1);
-      if (!mbar_wait(&bars[kBarOFinal], seg & 1, s_abort)) expired = true;
+      if (!mbar_wait(&bars[kBarPVDone + (it - 1) % kStages], ((it - 1) / kStages) & 1, s_abort)) expired = true;
       tc_fence_after();
       if (nparts == 1) {
         const int row0 = kRowBlock * g.rb + c0;

@@ -31,6 +31,45 @@ SPADE_DEVICE float ex2(float x) {
   return y;
 }
 
+// (a & mask) | bits in one instruction.
+SPADE_DEVICE uint32_t and_or(uint32_t a, uint32_t mask, uint32_t bits) {
+  uint32_t r;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(a), "r"(mask), "r"(bits));
+  return r;
+}
+
+// ---------------------------------------------------------------- fp32 pairs
+// Two fp32 operations per instruction, each rounded as its scalar form.
+struct F2 {
+  uint64_t v;
+};
+SPADE_DEVICE F2 f2(float lo, float hi) {
+  F2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(lo), "f"(hi));
+  return r;
+}
+SPADE_DEVICE void f2_split(F2 a, float &lo, float &hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(a.v)); }
+SPADE_DEVICE F2 f2_add(F2 a, F2 b) {
+  F2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+SPADE_DEVICE F2 f2_mul(F2 a, F2 b) {
+  F2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+SPADE_DEVICE F2 f2_fma(F2 a, F2 b, F2 c) {
+  F2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
+}
+SPADE_DEVICE float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+
 // ---------------------------------------------------------------- mbarrier
 SPADE_DEVICE void mbar_init(uint64_t *bar, uint32_t count) {
   asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(count));
@@ -108,6 +147,26 @@ SPADE_DEVICE bool mbar_wait_unabortable(uint64_t *bar, uint32_t parity) {
   const uint64_t t0 = globaltimer();
   while (!mbar_try_wait(bar, parity)) {
     if (globaltimer() - t0 > kWaitLimitNs) return false;
+  }
+  return true;
+}
+
+// The same for loops that look at the abort flag themselves, once per round.  A wait
+// that is over costs two instructions, and one that is not polls in four: the clock
+// and the flag are looked at after kLeanPolls polls only (each suspends the thread
+// for kSuspendNs at most).  Sets the flag when the limit passes.
+constexpr int kLeanPolls = 256;
+SPADE_DEVICE bool mbar_wait_lean(uint64_t *bar, uint32_t parity, volatile int *abort) {
+#pragma unroll 1
+  for (int i = 0; i < kLeanPolls; ++i)
+    if (mbar_try_wait(bar, parity)) return true;
+  const uint64_t t0 = globaltimer();
+  while (!mbar_try_wait(bar, parity)) {
+    if (*abort) return false;
+    if (globaltimer() - t0 > kWaitLimitNs) {
+      *abort = 1;
+      return false;
+    }
   }
   return true;
 }

@@ -24,6 +24,31 @@ SPADE_DEVICE float2 pair_of(uint32_t bits) {
   return __half22float2(h);
 }
 
+// A word's eight codes minus the zero, as four pairs of bf16 (exact): a code in the
+// low bits of the bf16 of 128 is 128 + code, and nz = -(128 + zero).
+SPADE_DEVICE void unpack_bf16(uint32_t w, __nv_bfloat162 nz, uint32_t *out) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const uint32_t u = and_or(w >> (4 * e), 0x000f000fu, 0x43004300u);
+    const __nv_bfloat162 v = __hadd2(*reinterpret_cast<const __nv_bfloat162 *>(&u), nz);
+    out[e] = *reinterpret_cast<const uint32_t *>(&v);
+  }
+}
+// The values in fp16: scale * (code - zero).  The float16 of 1024 holds a code in its
+// low bits, or 16 times one in the next: nz = -(1024 + zero), nz16 = -(64 + zero).
+SPADE_DEVICE void unpack_fp16(uint32_t w, __half2 s, __half2 nz, __half2 nz16, uint32_t *out) {
+  const __half2 sixteenth = __float2half2_rn(0.0625f);
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const uint32_t lo = and_or(w, 0x000f000fu, 0x64006400u), hi = and_or(w, 0x00f000f0u, 0x64006400u);
+    const __half2 a = __hmul2(__hadd2(*reinterpret_cast<const __half2 *>(&lo), nz), s);
+    const __half2 b = __hmul2(__hfma2(*reinterpret_cast<const __half2 *>(&hi), sixteenth, nz16), s);
+    out[2 * e] = *reinterpret_cast<const uint32_t *>(&a);
+    out[2 * e + 1] = *reinterpret_cast<const uint32_t *>(&b);
+    w >>= 8;
+  }
+}
+
 // The cache's pages (see include/spade.h).
 struct Cache {
   uint8_t *k_codes, *v_codes;

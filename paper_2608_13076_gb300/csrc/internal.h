@@ -45,11 +45,12 @@ bool encode_tmap_bf16_sw128_nd(CUtensorMap *map, const void *base, uint32_t rank
 bool encode_tmap_bf16_sw128(CUtensorMap *map, const void *base, uint64_t inner, uint64_t rows,
                             uint64_t row_stride_bytes, uint32_t box_inner, uint32_t box_rows);
 
-// Encodes a byte matrix [rows, row_bytes] of 64- or 32-byte rows, one after the
-// other, in boxes of box_rows whole rows whose 16-byte pieces are swizzled (64-byte
-// rows: piece j of row r at j ^ (r / 2) % 4; 32-byte rows: j ^ (r / 4) % 2); zeros
-// out of bounds.
-bool encode_tmap_bytes(CUtensorMap *map, const void *base, uint32_t row_bytes, uint64_t rows, uint32_t box_rows);
+// Encodes a byte matrix [rows, row_bytes] (row_bytes a multiple of 16) in boxes of
+// box_rows x box_bytes (64 or 32) whose 16-byte pieces are swizzled (64-byte boxes:
+// piece j of row r at j ^ (r / 2) % 4; 32-byte ones: j ^ (r / 4) % 2); zeros out of
+// bounds.
+bool encode_tmap_bytes(CUtensorMap *map, const void *base, uint32_t row_bytes, uint64_t rows, uint32_t box_rows,
+                       uint32_t box_bytes);
 // Encodes a matrix of 32-bit words [rows, row_words], one row per box, zeros out of bounds.
 bool encode_tmap_words(CUtensorMap *map, const void *base, uint32_t row_words, uint64_t rows);
 

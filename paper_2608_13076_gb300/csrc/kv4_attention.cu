@@ -69,8 +69,8 @@ extern "C" spade_status spade_verify_attention_kv4(
 
   const uint64_t rows = static_cast<uint64_t>(num_pages) * Hkv * page_size;
   CUtensorMap kc, vc, kp, vp;
-  if (!encode_tmap_bytes(&kc, k_codes, D / 2, rows, attn::kChunk) ||
-      !encode_tmap_bytes(&vc, v_codes, D / 2, rows, attn::kChunk) ||
+  if (!encode_tmap_bytes(&kc, k_codes, D / 2, rows, attn::kChunk, D / 2) ||
+      !encode_tmap_bytes(&vc, v_codes, D / 2, rows, attn::kChunk, D / 2) ||
       !encode_tmap_words(&kp, k_params, attn::kChunk * (D / 64), rows / attn::kChunk) ||
       !encode_tmap_words(&vp, v_params, attn::kChunk * (D / 64), rows / attn::kChunk))
     return SPADE_ERR_CUDA;

@@ -100,31 +100,6 @@ static_assert(Smem::V % 1024 == 0 && Smem::Q % 1024 == 0 && Smem::P % 1024 == 0 
 static_assert(Smem::BAR % 8 == 0 && Smem::RMAX % 16 == 0 && Smem::SCALE % 16 == 0, "alignment");
 static_assert(Smem::BYTES <= 227 * 1024, "shared memory budget");
 
-// A word's eight codes minus the zero, as four pairs of bf16 (exact): a code in the
-// low bits of the bf16 of 128 is 128 + code, and nz = -(128 + zero).
-SPADE_DEVICE void unpack_bf16(uint32_t w, __nv_bfloat162 nz, uint32_t *out) {
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const uint32_t u = and_or(w >> (4 * e), 0x000f000fu, 0x43004300u);
-    const __nv_bfloat162 v = __hadd2(*reinterpret_cast<const __nv_bfloat162 *>(&u), nz);
-    out[e] = *reinterpret_cast<const uint32_t *>(&v);
-  }
-}
-// The values in fp16: scale * (code - zero).  The float16 of 1024 holds a code in its
-// low bits, or 16 times one in the next: nz = -(1024 + zero), nz16 = -(64 + zero).
-SPADE_DEVICE void unpack_fp16(uint32_t w, __half2 s, __half2 nz, __half2 nz16, uint32_t *out) {
-  const __half2 sixteenth = __float2half2_rn(0.0625f);
-#pragma unroll
-  for (int e = 0; e < 2; ++e) {
-    const uint32_t lo = and_or(w, 0x000f000fu, 0x64006400u), hi = and_or(w, 0x00f000f0u, 0x64006400u);
-    const __half2 a = __hmul2(__hadd2(*reinterpret_cast<const __half2 *>(&lo), nz), s);
-    const __half2 b = __hmul2(__hfma2(*reinterpret_cast<const __half2 *>(&hi), sixteenth, nz16), s);
-    out[2 * e] = *reinterpret_cast<const uint32_t *>(&a);
-    out[2 * e + 1] = *reinterpret_cast<const uint32_t *>(&b);
-    w >>= 8;
-  }
-}
-
 SPADE_DEVICE bool finite_scale(uint32_t pair) { return (pair & 0x7c00u) != 0x7c00u; }
 
 // The (scale, zero) pairs of key t: one per group of 64 dims.
@@ -411,10 +386,10 @@ __global__ void __launch_bounds__(kThreads, 1)
           const uint4 v = load_codes<D>(stage, t, j);
           const __nv_bfloat162 nz = __float2bfloat162_rn(-128.f - int4::pair_of(kp[j / 2]).y);
           uint32_t a[16];
-          unpack_bf16(v.x, nz, a);
-          unpack_bf16(v.y, nz, a + 4);
-          unpack_bf16(v.z, nz, a + 8);
-          unpack_bf16(v.w, nz, a + 12);
+          int4::unpack_bf16(v.x, nz, a);
+          int4::unpack_bf16(v.y, nz, a + 4);
+          int4::unpack_bf16(v.z, nz, a + 8);
+          int4::unpack_bf16(v.w, nz, a + 12);
           tmem_st16(tmem + (static_cast<uint32_t>(q4 * 32) << 16) + kColK + st * (D / 2) + j * 16, a);
         }
         // The scales that the scores take, in log2 units: NaN where the key's or the value's is not finite.
@@ -445,7 +420,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             uint32_t h[4];
-            unpack_fp16(w[i], s, nz, nz16, h);
+            int4::unpack_fp16(w[i], s, nz, nz16, h);
             *reinterpret_cast<uint4 *>(row + (j / 2) * kSlab + ((((j % 2) * 4 + i) ^ (t & 7)) << 4)) =
                 make_uint4(h[0], h[1], h[2], h[3]);
           }

@@ -105,10 +105,11 @@ bool encode_tmap_bf16_sw128_nd(CUtensorMap *map, const void *base, uint32_t rank
                      box);
 }
 
-bool encode_tmap_bytes(CUtensorMap *map, const void *base, uint32_t row_bytes, uint64_t rows, uint32_t box_rows) {
+bool encode_tmap_bytes(CUtensorMap *map, const void *base, uint32_t row_bytes, uint64_t rows, uint32_t box_rows,
+                       uint32_t box_bytes) {
   const uint64_t dims[2] = {row_bytes, rows}, strides[1] = {row_bytes};
-  const uint32_t box[2] = {row_bytes, box_rows};
-  return encode_tmap(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, row_bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B
+  const uint32_t box[2] = {box_bytes, box_rows};
+  return encode_tmap(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, box_bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B
                                                                         : CU_TENSOR_MAP_SWIZZLE_32B,
                      base, 2, dims, strides, box);
 }

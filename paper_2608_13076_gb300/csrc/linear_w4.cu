@@ -16,7 +16,8 @@ struct Params {
   __nv_bfloat16 *out;
   int32_t *status;
   int R, N, K;
-  int tile_rows, split;  // (more than eight rows) rows of a tile; CTAs that share a tile's units
+  // (More than eight rows) rows of a tile, rounded up to 16, and the CTAs that share its units.
+  int tile_rows, tile_n, split;
 };
 
 // ---- up to eight rows: the weights streamed past mma.sync -----------------------------------
@@ -212,46 +213,57 @@ __global__ void __launch_bounds__(kThreads) few_rows_kernel(const __grid_constan
 }
 
 // ---- more rows: tcgen05 with the weights in tensor memory ----------------------------------
-// y^T = W x^T again: 128 outputs on M, up to 64 rows of x on N, units of 128 k.  A thread
-// unpacks one output's unit (64 bytes of codes) to whole numbers in bf16 and stores them
-// to its lane of tensor memory, from where the MMA takes A (no shared-memory traffic for
-// W beyond its codes, and no loss of MMA rate at small N); x comes by TMA as B.  Each
+// y^T = W x^T again: 128 outputs on M, up to 128 rows of x on N, units of 128 k.  Two
+// threads unpack one output's unit (64 bytes of codes) to whole numbers in bf16 and store
+// them to its lane of tensor memory, from where the MMA takes A (no shared-memory traffic
+// for W beyond its codes, and no loss of MMA rate at small N); x comes by TMA as B.  Each
 // group of k is accumulated apart, exact but for the fp32 sums, in one of two blocks of
-// columns, and four warps drain the other under the outputs' scales into registers.
-// Bound by the weights' bytes up to ~50 rows, by the unpacking's and draining's
-// instructions and the MMAs (which share a unit about evenly at 64 rows) beyond.
-// Two CTAs share an SM, so one's waits are the other's work.  Where the tiles do not fill
-// the GPU, a cluster of 2, 4 or 8 CTAs takes a tile's units in equal parts and adds the
-// sums through distributed shared memory in a fixed order.
+// columns, and the draining warps take the other under the outputs' scales into registers.
+// Bound by the weights' bytes at few rows, then by the instructions that unpack (each row
+// tile unpacks W again) and drain, with the MMAs close behind at 128 rows.  Up to 32 rows
+// a tile two CTAs share an SM, so that one's waits are the other's work; wider tiles take
+// an SM each, since halving the unpacking is worth more (389 rows of 7168 x 5120 in tiles
+// of 56 rows, two CTAs: 99 us).
+// Where the tiles do not fill the GPU, a cluster of 2, 4 or 8 CTAs takes a tile's units
+// in equal parts and adds the sums through distributed shared memory in a fixed order.
 namespace tc {
 
 constexpr int kOut = 128;                       // outputs of a tile
-constexpr int kStages = 4;                      // copy ring (units)
-constexpr int kThreads = 320;                   // copies, MMA, four draining and four unpacking warps
-constexpr int kWarpDrain = 2, kWarpUnpack = 6;
 constexpr int kCodes = kOut * 64;               // a unit's codes: 8 KB
-constexpr uint32_t kTmemCols = 256;             // sums: two blocks of 64 columns; weights: two of 64
-constexpr uint32_t kColD = 0, kColA = 128;
 constexpr int kMaxSplit = 8;
+constexpr int kMaxStages = 6, kMaxA = 4;
 
-template <int NR>
-struct Smem {
-  static constexpr int kX = NR * 256;           // a unit of x: two slabs of [NR][64 k]
+template <bool kWide>
+struct Shape {
+  static constexpr int kRows = kWide ? 128 : 32;       // most rows of a tile
+  static constexpr int kHalves = kWide ? 2 : 1;        // draining warps per lane quadrant
+  static constexpr int kHalfRows = kRows / kHalves;    // sums of a draining thread
+  static constexpr int kWarpDrain = 2, kWarpUnpack = 2 + 4 * kHalves;
+  static constexpr int kThreads = 32 * (kWarpUnpack + 8);
+  static constexpr int kPerSm = kWide ? 1 : 2;
+  static constexpr int kStages = kWide ? 5 : 6;        // copy ring (units)
+  static constexpr int kA = kWide ? 4 : 3;             // unpacked units
+  static constexpr uint32_t kTmemCols = kWide ? 512 : 256;
+  static constexpr uint32_t kColD = 0, kColA = 2 * kRows;
+  static constexpr int kX = kRows * 256;               // a unit of x: two slabs of [rows][64 k]
   static constexpr int kStage = kCodes + kX;
-  static constexpr int kSums = kOut * NR * 4;   // the split's sums reuse the ring
-  static constexpr int RING = 0;
-  static constexpr int BYTES = (kStages * kStage > kSums ? kStages * kStage : kSums) + 1024;
+  static constexpr int kBytes = kStages * kStage + 1024;
+  static_assert(kColA + kA * 64 <= kTmemCols, "tensor memory");
+  static_assert(kOut * kRows * 4 <= kStages * kStage, "a split's sums reuse the ring");
+  static_assert(kStages <= kMaxStages && kA <= kMaxA, "barriers");
 };
 
-template <int G, int NR>
-__global__ void __launch_bounds__(kThreads, 2) rows_kernel(const __grid_constant__ Params p,
-                                                           const __grid_constant__ CUtensorMap tm_w,
-                                                           const __grid_constant__ CUtensorMap tm_x) {
+template <int G, bool kWide>
+__global__ void __launch_bounds__(Shape<kWide>::kThreads, Shape<kWide>::kPerSm)
+    rows_kernel(const __grid_constant__ Params p, const __grid_constant__ CUtensorMap tm_w,
+                const __grid_constant__ CUtensorMap tm_x) {
+  using S = Shape<kWide>;
   constexpr int U = kUnit / G;
-  using S = Smem<NR>;
+  constexpr int kBlocks = S::kHalfRows / 16;  // blocks of 16 rows of a draining thread
   extern __shared__ uint8_t smem_raw[];
   uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-  __shared__ uint64_t s_full[kStages], s_empty[kStages], s_afull[2], s_afree[2], s_dfull[2], s_dfree[2], s_drain;
+  __shared__ uint64_t s_full[kMaxStages], s_empty[kMaxStages], s_afull[kMaxA], s_afree[kMaxA], s_dfull[2], s_dfree[2],
+      s_drain;
   __shared__ int s_abort;
   __shared__ uint32_t s_tmem;
   const int warp = uniform_warp(), lane = threadIdx.x & 31;
@@ -259,21 +271,23 @@ __global__ void __launch_bounds__(kThreads, 2) rows_kernel(const __grid_constant
     s_abort = 0;
     tma_prefetch_desc(&tm_w);
     tma_prefetch_desc(&tm_x);
-    for (int s = 0; s < kStages; ++s) {
+    for (int s = 0; s < S::kStages; ++s) {
       mbar_init(&s_full[s], 1);
-      mbar_init(&s_empty[s], 5);  // four unpacking warps and the MMAs
+      mbar_init(&s_empty[s], 9);  // eight unpacking warps and the MMAs
+    }
+    for (int s = 0; s < S::kA; ++s) {
+      mbar_init(&s_afull[s], 8);
+      mbar_init(&s_afree[s], 1);
     }
     for (int s = 0; s < 2; ++s) {
-      mbar_init(&s_afull[s], 4);
-      mbar_init(&s_afree[s], 1);
       mbar_init(&s_dfull[s], 1);
-      mbar_init(&s_dfree[s], 4);
+      mbar_init(&s_dfree[s], 4 * S::kHalves);
     }
     mbar_init(&s_drain, 1);
     fence_mbar_init();
   }
   if (warp == 1) {
-    tmem_alloc(&s_tmem, kTmemCols);
+    tmem_alloc(&s_tmem, S::kTmemCols);
     tmem_relinquish();
   }
   tc_fence_before();
@@ -283,35 +297,44 @@ __global__ void __launch_bounds__(kThreads, 2) rows_kernel(const __grid_constant
   const int groups = p.K / G, units = (groups + U - 1) / U;
   const int split = p.split, rank = split > 1 ? static_cast<int>(cluster_ctarank()) : 0;
   const int o0 = static_cast<int>(blockIdx.x / split) * kOut, n0 = blockIdx.y * p.tile_rows;
+  const int n = p.tile_n;  // rows of x in the MMA: the tile's, rounded up to 16
   const int u0 = static_cast<int>(static_cast<int64_t>(units) * rank / split);
   const int u1 = static_cast<int>(static_cast<int64_t>(units) * (rank + 1) / split);
+  const int t = (warp & 3) * 32 + lane;                       // output of the unpacking and draining threads
+  const uint32_t tlane = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
+  const uint32_t *pair = p.pairs + static_cast<int64_t>(min(o0 + t, p.N - 1)) * groups;
+  const bool whole = groups % U == 0;
+  const int half_rows = kWide ? (n / 16 + 1) / 2 * 16 : n;    // rows of the first draining half
+  const int r_lo = kWide && warp >= S::kWarpDrain + 4 ? half_rows : 0;  // this thread's first row (draining)
+  const int my_rows = min(half_rows, n - r_lo);
   griddep_wait();
   griddep_launch_dependents();
-  float acc[NR];  // (draining warps: one output's sums)
+  F2 sum[S::kHalfRows / 2];  // (draining warps: one output's sums)
   bool ok = true;
   if (warp == 0) {
     // ---- copies ----
     const bool leader = elect_one();
-    const uint64_t once = l2_policy_evict_first(), again = l2_policy_evict_last();
+    // x is read by every tile of outputs, W again by every tile of rows.
+    const uint64_t pol = l2_policy_evict_last(), pol_w = gridDim.y > 1 ? pol : l2_policy_evict_first();
     uint32_t issued = 0;
     for (int u = u0; u < u1; ++u, ++issued) {
-      const int st = issued % kStages;
-      ok = __all_sync(0xffffffffu, mbar_wait_lean(&s_empty[st], ((issued / kStages) & 1) ^ 1, &s_abort));
+      const int st = issued % S::kStages;
+      ok = __all_sync(0xffffffffu, mbar_wait_lean(&s_empty[st], ((issued / S::kStages) & 1) ^ 1, &s_abort));
       if (!ok) break;
       uint8_t *stage = smem + st * S::kStage;
       if (leader) {
-        mbar_arrive_expect_tx(&s_full[st], S::kStage);
-        tma_load_2d(stage, &tm_w, u * (kUnit / 2), o0, &s_full[st], once);
-        tma_load_2d(stage + kCodes, &tm_x, u * kUnit, n0, &s_full[st], again);
-        tma_load_2d(stage + kCodes + S::kX / 2, &tm_x, u * kUnit + 64, n0, &s_full[st], again);
+        mbar_arrive_expect_tx(&s_full[st], kCodes + n * 256);
+        tma_load_2d(stage, &tm_w, u * (kUnit / 2), o0, &s_full[st], pol_w);
+        tma_load_2d(stage + kCodes, &tm_x, u * kUnit, n0, &s_full[st], pol);
+        tma_load_2d(stage + kCodes + S::kX / 2, &tm_x, u * kUnit + 64, n0, &s_full[st], pol);
       }
     }
     if (!ok && leader)  // every copy issued must land before the CTA's shared memory goes away
-      for (uint32_t j = issued > kStages ? issued - kStages : 0; j < issued; ++j)
-        mbar_wait_unabortable(&s_full[j % kStages], (j / kStages) & 1);
+      for (uint32_t j = issued > S::kStages ? issued - S::kStages : 0; j < issued; ++j)
+        mbar_wait_unabortable(&s_full[j % S::kStages], (j / S::kStages) & 1);
   } else if (warp == 1) {
     // ---- MMAs ----
-    constexpr uint32_t idesc = idesc_bf16_f32(kOut, NR);
+    const uint32_t idesc = idesc_bf16_f32(kOut, n);
     const bool leader = elect_one();
     const uint32_t base = smem_u32(smem);
     uint32_t it = 0, gi = 0;
@@ -319,9 +342,9 @@ __global__ void __launch_bounds__(kThreads, 2) rows_kernel(const __grid_constant
       ok = __all_sync(0xffffffffu, mbar_wait_lean(bar, parity, &s_abort)) && ok;
     };
     for (int u = u0; ok && u < u1; ++u, ++it) {
-      const int st = it % kStages, as = it & 1;
-      wait(&s_full[st], (it / kStages) & 1);
-      wait(&s_afull[as], (it / 2) & 1);
+      const int st = it % S::kStages, as = it % S::kA;
+      wait(&s_full[st], (it / S::kStages) & 1);
+      wait(&s_afull[as], (it / S::kA) & 1);
       if (!ok) break;
       const uint64_t dx = smem_desc_sw128(base + st * S::kStage + kCodes);
       const int ng = min(U, groups - u * U);
@@ -333,10 +356,10 @@ __global__ void __launch_bounds__(kThreads, 2) rows_kernel(const __grid_constant
         tc_fence_after();
 #pragma unroll
         for (int k = 0; k < G / 16; ++k) {
-          constexpr int kSlabSteps = 4;  // MMAs per 64-k slab
-          const int kk = q * (G / 16) + k;
-          const uint32_t off = ((kk / kSlabSteps) * (S::kX / 2) + (kk % kSlabSteps) * 32) >> 4;
-          if (leader) tc_mma_f16_ta(tmem + kColD + db * 64, tmem + kColA + as * 64 + kk * 8, dx + off, idesc, k > 0);
+          const int kk = q * (G / 16) + k;  // four per 64-k slab
+          const uint32_t off = ((kk / 4) * (S::kX / 2) + (kk % 4) * 32) >> 4;
+          if (leader)
+            tc_mma_f16_ta(tmem + S::kColD + db * S::kRows, tmem + S::kColA + as * 64 + kk * 8, dx + off, idesc, k > 0);
         }
         if (leader) tc_commit(&s_dfull[db]);
         ++gi;
@@ -351,36 +374,33 @@ __global__ void __launch_bounds__(kThreads, 2) rows_kernel(const __grid_constant
       tc_commit(&s_drain);
       mbar_wait_unabortable(&s_drain, 0);
     }
-  } else if (warp >= kWarpUnpack) {
-    // ---- unpacking: a thread per output ----
-    const int t = (warp & 3) * 32 + lane;
-    const uint32_t taddr = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + kColA;
-    const uint32_t *pair = p.pairs + static_cast<int64_t>(min(o0 + t, p.N - 1)) * groups;
-    const bool whole = groups % U == 0;
-    uint32_t now[U], next[U];
-    if (u0 < u1) load_unit_pairs<U>(pair, u0, groups, whole, next);
+  } else if (warp >= S::kWarpUnpack) {
+    // ---- unpacking: two threads per output, 64 k each ----
+    const int part = (warp - S::kWarpUnpack) / 4;
+    uint32_t pr[2][U];
+    if (u0 < u1) load_unit_pairs<U>(pair, u0, groups, whole, pr[0]);
     uint32_t it = 0;
-    for (int u = u0; u < u1; ++u, ++it) {
-#pragma unroll
-      for (int q = 0; q < U; ++q) now[q] = next[q];
+    auto unit = [&](int u, const uint32_t (&now)[U], uint32_t (&next)[U]) {
       if (u + 1 < u1) load_unit_pairs<U>(pair, u + 1, groups, whole, next);
-      const int st = it % kStages, as = it & 1;
-      ok = mbar_wait_lean(&s_full[st], (it / kStages) & 1, &s_abort) &&
-           mbar_wait_lean(&s_afree[as], ((it / 2) & 1) ^ 1, &s_abort);
+      const int st = it % S::kStages, as = it % S::kA;
+      ok = mbar_wait_lean(&s_full[st], (it / S::kStages) & 1, &s_abort) &&
+           mbar_wait_lean(&s_afree[as], ((it / S::kA) & 1) ^ 1, &s_abort);
       ok = __all_sync(0xffffffffu, ok);
-      if (!ok) break;
+      if (!ok) return;
       tc_fence_after();
       const uint8_t *row = smem + st * S::kStage + t * 64;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
+      for (int h = 0; h < 2; ++h) {
+        const int j = 2 * part + h;  // 32 k
         const uint4 v = *reinterpret_cast<const uint4 *>(row + ((j ^ ((t >> 1) & 3)) << 4));
-        const __nv_bfloat162 nz = __float2bfloat162_rn(-128.f - int4::pair_of(now[j * 32 / G]).y);
+        const uint32_t pair_bits = U == 1 ? now[0] : U == 2 ? (part ? now[U - 1] : now[0]) : (part ? now[(2 + h) % U] : now[h % U]);
+        const __nv_bfloat162 nz = __float2bfloat162_rn(-128.f - int4::pair_of(pair_bits).y);
         uint32_t a[16];
         int4::unpack_bf16(v.x, nz, a);
         int4::unpack_bf16(v.y, nz, a + 4);
         int4::unpack_bf16(v.z, nz, a + 8);
         int4::unpack_bf16(v.w, nz, a + 12);
-        tmem_st16(taddr + as * 64 + j * 16, a);
+        tmem_st16(tlane + S::kColA + as * 64 + j * 16, a);
       }
       tmem_wait_st();
       tc_fence_before();
@@ -389,22 +409,20 @@ __global__ void __launch_bounds__(kThreads, 2) rows_kernel(const __grid_constant
         mbar_arrive(&s_afull[as]);
         mbar_arrive(&s_empty[st]);
       }
+      ++it;
+    };
+    for (int u = u0; ok && u < u1; u += 2) {
+      unit(u, pr[0], pr[1]);
+      if (ok && u + 1 < u1) unit(u + 1, pr[1], pr[0]);
     }
   } else {
     // ---- draining: a group's sums under the outputs' scales ----
-    const int t = (warp & 3) * 32 + lane;
-    const uint32_t taddr = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + kColD;
-    const uint32_t *pair = p.pairs + static_cast<int64_t>(min(o0 + t, p.N - 1)) * groups;
-    const bool whole = groups % U == 0;
-    uint32_t now[U], next[U];
-    if (u0 < u1) load_unit_pairs<U>(pair, u0, groups, whole, next);
-    F2 sum[NR / 2];
+    uint32_t pr[2][U];
+    if (u0 < u1) load_unit_pairs<U>(pair, u0, groups, whole, pr[0]);
 #pragma unroll
-    for (int r = 0; r < NR / 2; ++r) sum[r] = f2(0.f, 0.f);
+    for (int r = 0; r < S::kHalfRows / 2; ++r) sum[r] = f2(0.f, 0.f);
     uint32_t gi = 0;
-    for (int u = u0; ok && u < u1; ++u) {
-#pragma unroll
-      for (int q = 0; q < U; ++q) now[q] = next[q];
+    auto unit = [&](int u, const uint32_t (&now)[U], uint32_t (&next)[U]) {
       if (u + 1 < u1) load_unit_pairs<U>(pair, u + 1, groups, whole, next);
       const int ng = min(U, groups - u * U);
 #pragma unroll
@@ -412,41 +430,46 @@ __global__ void __launch_bounds__(kThreads, 2) rows_kernel(const __grid_constant
         if (q >= ng) break;
         const int db = gi & 1;
         ok = __all_sync(0xffffffffu, mbar_wait_lean(&s_dfull[db], (gi / 2) & 1, &s_abort));
-        if (!ok) break;
+        if (!ok) return;
         tc_fence_after();
         const float s = int4::pair_of(now[q]).x;
         const F2 ss = f2(s, s);
+        const uint32_t from = tlane + S::kColD + db * S::kRows + r_lo;
 #pragma unroll
-        for (int r = 0; r < NR; r += 16) {
+        for (int k = 0; k < kBlocks; ++k) {
+          if (k * 16 >= my_rows) break;
           uint32_t y[16];
-          tmem_ld8(taddr + db * 64 + r, y);
-          tmem_ld8(taddr + db * 64 + r + 8, y + 8);
+          tmem_ld8(from + k * 16, y);
+          tmem_ld8(from + k * 16 + 8, y + 8);
           tmem_wait_ld();
 #pragma unroll
           for (int e = 0; e < 16; e += 2)
-            sum[(r + e) / 2] = f2_fma(f2(__uint_as_float(y[e]), __uint_as_float(y[e + 1])), ss, sum[(r + e) / 2]);
+            sum[k * 8 + e / 2] = f2_fma(f2(__uint_as_float(y[e]), __uint_as_float(y[e + 1])), ss, sum[k * 8 + e / 2]);
         }
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&s_dfree[db]);
         ++gi;
       }
+    };
+    for (int u = u0; ok && u < u1; u += 2) {
+      unit(u, pr[0], pr[1]);
+      if (ok && u + 1 < u1) unit(u + 1, pr[1], pr[0]);
     }
-#pragma unroll
-    for (int r = 0; r < NR; r += 2) f2_split(sum[r / 2], acc[r], acc[r + 1]);
   }
   if (!ok && lane == 0) atomicOr(p.status, SPADE_DEV_TIMEOUT);
 
   const int rows = min(p.tile_rows, p.R - n0);
-  const bool drains = warp >= kWarpDrain && warp < kWarpUnpack;
-  const int t = (warp & 3) * 32 + lane;
+  const bool drains = warp >= S::kWarpDrain && warp < S::kWarpUnpack;
   if (split == 1) {
     if (drains && o0 + t < p.N) {
 #pragma unroll
-      for (int r = 0; r < NR; ++r) {
-        if (r >= rows) break;
-        const int64_t at = static_cast<int64_t>(n0 + r) * p.N + o0 + t;
-        p.out[at] = __float2bfloat16_rn(acc[r] + (p.residual ? __bfloat162float(p.residual[at]) : 0.f));
+      for (int r = 0; r < S::kHalfRows; ++r) {
+        if (r >= my_rows || r_lo + r >= rows) break;
+        float y[2];
+        f2_split(sum[r / 2], y[0], y[1]);
+        const int64_t at = static_cast<int64_t>(n0 + r_lo + r) * p.N + o0 + t;
+        p.out[at] = __float2bfloat16_rn(y[r & 1] + (p.residual ? __bfloat162float(p.residual[at]) : 0.f));
       }
     }
   } else {
@@ -456,23 +479,33 @@ __global__ void __launch_bounds__(kThreads, 2) rows_kernel(const __grid_constant
     __syncthreads();
     if (drains) {
 #pragma unroll
-      for (int r = 0; r < NR; ++r) sums[r * kOut + t] = acc[r];
+      for (int r = 0; r < S::kHalfRows; r += 2) {
+        if (r >= my_rows) break;
+        float y[2];
+        f2_split(sum[r / 2], y[0], y[1]);
+        sums[(r_lo + r) * kOut + t] = y[0];
+        sums[(r_lo + r + 1) * kOut + t] = y[1];
+      }
     }
     __syncwarp();
     cluster_sync();
     const int r0 = rows * rank / split, r1 = rows * (rank + 1) / split;
-    for (int e = threadIdx.x; e < (r1 - r0) * kOut; e += kThreads) {
-      const int r = r0 + e / kOut, o = e % kOut;
-      float y = 0.f;
+    for (int e = threadIdx.x; e < (r1 - r0) * (kOut / 4); e += S::kThreads) {
+      const int r = r0 + e / (kOut / 4), o = e % (kOut / 4) * 4;
+      float y[4] = {};
       for (int c = 0; c < split; ++c) {
-        float v;
-        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(cluster_map(sums + r * kOut + o, c)));
-        y += v;
+        float v[4];
+        asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                     : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3])
+                     : "r"(cluster_map(sums + r * kOut + o, c)));
+#pragma unroll
+        for (int k = 0; k < 4; ++k) y[k] += v[k];
       }
-      if (o0 + o < p.N) {
-        const int64_t at = static_cast<int64_t>(n0 + r) * p.N + o0 + o;
-        p.out[at] = __float2bfloat16_rn(y + (p.residual ? __bfloat162float(p.residual[at]) : 0.f));
-      }
+      const int64_t at = static_cast<int64_t>(n0 + r) * p.N + o0 + o;
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (o0 + o + k < p.N)
+          p.out[at + k] = __float2bfloat16_rn(y[k] + (p.residual ? __bfloat162float(p.residual[at + k]) : 0.f));
     }
     __syncwarp();
     cluster_sync();  // no CTA leaves while another reads its sums
@@ -481,7 +514,7 @@ __global__ void __launch_bounds__(kThreads, 2) rows_kernel(const __grid_constant
   __syncthreads();
   if (warp == 1) {
     tc_fence_after();
-    tmem_dealloc(tmem, kTmemCols);
+    tmem_dealloc(tmem, S::kTmemCols);
   }
 }
 
@@ -523,32 +556,24 @@ static cudaError_t few_rows(const Params &p, const CUtensorMap &tm, bool wide, c
   return wide ? few_rows_mt<G, 2>(p, tm, s) : few_rows_mt<G, 1>(p, tm, s);
 }
 
-template <int G, int NR>
-static cudaError_t rows_nr(const Params &p, const CUtensorMap &w, const CUtensorMap &x, cudaStream_t s) {
+template <int G, bool kWide>
+static cudaError_t rows(const Params &p, const CUtensorMap &w, const CUtensorMap &x, cudaStream_t s) {
+  using S = tc::Shape<kWide>;
   static OncePerDevice once;
-  const cudaError_t e = set_max_smem(once, tc::Smem<NR>::BYTES, tc::rows_kernel<G, NR>);
+  const cudaError_t e = set_max_smem(once, S::kBytes, tc::rows_kernel<G, kWide>);
   if (e != cudaSuccess) return e;
   const unsigned tiles = (static_cast<unsigned>(p.N) + tc::kOut - 1) / tc::kOut;
   const dim3 grid(tiles * p.split, (p.R + p.tile_rows - 1) / p.tile_rows);
-  return launch(tc::rows_kernel<G, NR>, grid, p.split, tc::kThreads, tc::Smem<NR>::BYTES, s, p, w, x);
-}
-template <int G>
-static cudaError_t rows_g(const Params &p, int nr, const CUtensorMap &w, const CUtensorMap &x, cudaStream_t s) {
-  switch (nr) {
-    case 16: return rows_nr<G, 16>(p, w, x, s);
-    case 32: return rows_nr<G, 32>(p, w, x, s);
-    case 48: return rows_nr<G, 48>(p, w, x, s);
-    default: return rows_nr<G, 64>(p, w, x, s);
-  }
+  return launch(tc::rows_kernel<G, kWide>, grid, p.split, S::kThreads, S::kBytes, s, p, w, x);
 }
 
-// CTAs that share a tile's units: those that fill the GPU's slots (two per SM) in the
-// fewest rounds per part, of at least four units each; the fewer the better.
-static int split_of(int64_t tiles, int units, int sms) {
+// CTAs that share a tile's units: those that fill the GPU's slots in the fewest rounds
+// per part, of at least four units each; the fewer the better.
+static int split_of(int64_t tiles, int units, int slots) {
   int best = 1;
   double cost = 1e30;
   for (int s = 1; s <= tc::kMaxSplit && (s == 1 || units >= 4 * s); s *= 2) {
-    const double c = static_cast<double>((tiles * s + 2 * sms - 1) / (2 * sms)) / s;
+    const double c = static_cast<double>((tiles * s + slots - 1) / slots) / s;
     if (c < cost) {
       cost = c;
       best = s;
@@ -583,7 +608,7 @@ extern "C" spade_status spade_linear_w4(const void *x, const void *codes, const 
   p.pairs = static_cast<const uint32_t *>(params);
   p.out = static_cast<__nv_bfloat16 *>(out);
   p.status = status;
-  p.R = R; p.N = N; p.K = K; p.tile_rows = R; p.split = 1;
+  p.R = R; p.N = N; p.K = K; p.tile_rows = p.tile_n = R; p.split = 1;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   CUtensorMap w;
   cudaError_t e;
@@ -594,19 +619,26 @@ extern "C" spade_status spade_linear_w4(const void *x, const void *codes, const 
         : group == 64 ? w4::few_rows<64>(p, w, wide, s)
                       : w4::few_rows<32>(p, w, wide, s);
   } else {
-    const int64_t row_tiles = (static_cast<int64_t>(R) + 63) / 64;
-    if (row_tiles > 65535) return fail(SPADE_ERR_SHAPE, "spade_linear_w4: R = %d exceeds %d rows per call", R, 65535 * 64);
-    p.tile_rows = static_cast<int>((R + row_tiles - 1) / row_tiles);
-    const int nr = (p.tile_rows + 15) / 16 * 16;
+    const bool wide = R > w4::tc::Shape<false>::kRows;
+    const int most = wide ? w4::tc::Shape<true>::kRows : w4::tc::Shape<false>::kRows;
+    const int row_tiles = (R - 1) / most + 1;
+    if (row_tiles > 65535) return fail(SPADE_ERR_SHAPE, "spade_linear_w4: R = %d exceeds %d rows per call", R, 65535 * most);
+    p.tile_rows = (R - 1) / row_tiles + 1;
+    p.tile_n = (p.tile_rows + 15) / 16 * 16;
     const int64_t tiles = (static_cast<int64_t>(N) + w4::tc::kOut - 1) / w4::tc::kOut * row_tiles;
-    p.split = w4::split_of(tiles, (K + w4::kUnit - 1) / w4::kUnit, sms);
+    p.split = w4::split_of(tiles, (K + w4::kUnit - 1) / w4::kUnit, wide ? sms : 2 * sms);
     CUtensorMap xm;
     if (!encode_tmap_bytes(&w, codes, K / 2, N, w4::tc::kOut, 64) ||
-        !encode_tmap_bf16_sw128(&xm, x, K, R, static_cast<uint64_t>(K) * 2, 64, nr))
+        !encode_tmap_bf16_sw128(&xm, x, K, R, static_cast<uint64_t>(K) * 2, 64, p.tile_n))
       return SPADE_ERR_CUDA;
-    e = group == 128 ? w4::rows_g<128>(p, nr, w, xm, s)
-        : group == 64 ? w4::rows_g<64>(p, nr, w, xm, s)
-                      : w4::rows_g<32>(p, nr, w, xm, s);
+    if (wide)
+      e = group == 128 ? w4::rows<128, true>(p, w, xm, s)
+          : group == 64 ? w4::rows<64, true>(p, w, xm, s)
+                        : w4::rows<32, true>(p, w, xm, s);
+    else
+      e = group == 128 ? w4::rows<128, false>(p, w, xm, s)
+          : group == 64 ? w4::rows<64, false>(p, w, xm, s)
+                        : w4::rows<32, false>(p, w, xm, s);
   }
   return e == cudaSuccess ? SPADE_OK : cuda_fail(e, "linear_w4 launch");
 }

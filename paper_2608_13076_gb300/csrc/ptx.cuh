@@ -151,12 +151,13 @@ SPADE_DEVICE bool mbar_wait_unabortable(uint64_t *bar, uint32_t parity) {
   return true;
 }
 
-// The same for loops that look at the abort flag themselves, once per round.  A wait
-// that is over costs two instructions, and one that is not polls in four: the clock
-// and the flag are looked at after kLeanPolls polls only (each suspends the thread
-// for kSuspendNs at most).  Sets the flag when the limit passes.
+// The same with little else in its loop: a wait that is over costs one test (15
+// cycles; a try_wait with its hint 50 to 100), and one that is not looks at the clock and
+// the abort flag after kLeanPolls polls only (each suspends the thread for kSuspendNs
+// at most).  Sets the flag when the limit passes.
 constexpr int kLeanPolls = 256;
 SPADE_DEVICE bool mbar_wait_lean(uint64_t *bar, uint32_t parity, volatile int *abort) {
+  if (mbar_test_wait(bar, parity)) return true;
 #pragma unroll 1
   for (int i = 0; i < kLeanPolls; ++i)
     if (mbar_try_wait(bar, parity)) return true;

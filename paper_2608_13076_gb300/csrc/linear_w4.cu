@@ -231,35 +231,51 @@ namespace tc {
 constexpr int kOut = 128;                       // outputs of a tile
 constexpr int kCodes = kOut * 64;               // a unit's codes: 8 KB
 constexpr int kMaxSplit = 8;
+constexpr int kNarrow = 32, kMost = 128;        // rows of a narrow and of a wide tile, at most
 constexpr int kMaxStages = 6, kMaxA = 4;
 
-template <bool kWide>
+template <int G, bool kWide>
 struct Shape {
-  static constexpr int kRows = kWide ? 128 : 32;       // most rows of a tile
+  static constexpr int kRows = kWide ? kMost : kNarrow;  // most rows of a tile
   static constexpr int kHalves = kWide ? 2 : 1;        // draining warps per lane quadrant
   static constexpr int kHalfRows = kRows / kHalves;    // sums of a draining thread
   static constexpr int kWarpDrain = 2, kWarpUnpack = 2 + 4 * kHalves;
   static constexpr int kThreads = 32 * (kWarpUnpack + 8);
   static constexpr int kPerSm = kWide ? 1 : 2;
-  static constexpr int kStages = kWide ? 5 : 6;        // copy ring (units)
-  static constexpr int kA = kWide ? 4 : 3;             // unpacked units
+  static constexpr int kStages = 5;                    // copy ring (units)
+  static constexpr int kBlock = !kWide && G <= 64 ? 2 : 1;  // groups accumulated side by side and drained together
+  static constexpr int kA = kWide ? 4 : kBlock == 2 ? 2 : 3;  // unpacked units
   static constexpr uint32_t kTmemCols = kWide ? 512 : 256;
-  static constexpr uint32_t kColD = 0, kColA = 2 * kRows;
+  static constexpr uint32_t kColD = 0, kColA = 2 * kBlock * kRows;
   static constexpr int kX = kRows * 256;               // a unit of x: two slabs of [rows][64 k]
-  static constexpr int kStage = kCodes + kX;
+  static constexpr int kPairs = kOut * (kUnit / G) * 4;  // a unit's (scale, zero) pairs
+  static constexpr int kStage = (kCodes + kX + kPairs + 1023) / 1024 * 1024;
   static constexpr int kBytes = kStages * kStage + 1024;
   static_assert(kColA + kA * 64 <= kTmemCols, "tensor memory");
   static_assert(kOut * kRows * 4 <= kStages * kStage, "a split's sums reuse the ring");
   static_assert(kStages <= kMaxStages && kA <= kMaxA, "barriers");
 };
 
+// Output t's pairs of a unit.
+template <int U>
+SPADE_DEVICE void read_pairs(const uint8_t *pairs, int t, uint32_t (&p)[U]) {
+  if constexpr (U == 4) {
+    const uint4 v = reinterpret_cast<const uint4 *>(pairs)[t];
+    p[0] = v.x; p[1] = v.y; p[2] = v.z; p[3] = v.w;
+  } else if constexpr (U == 2) {
+    const uint2 v = reinterpret_cast<const uint2 *>(pairs)[t];
+    p[0] = v.x; p[1] = v.y;
+  } else {
+    p[0] = reinterpret_cast<const uint32_t *>(pairs)[t];
+  }
+}
+
 template <int G, bool kWide>
-__global__ void __launch_bounds__(Shape<kWide>::kThreads, Shape<kWide>::kPerSm)
+__global__ void __launch_bounds__(Shape<G, kWide>::kThreads, Shape<G, kWide>::kPerSm)
     rows_kernel(const __grid_constant__ Params p, const __grid_constant__ CUtensorMap tm_w,
                 const __grid_constant__ CUtensorMap tm_x) {
-  using S = Shape<kWide>;
+  using S = Shape<G, kWide>;
   constexpr int U = kUnit / G;
-  constexpr int kBlocks = S::kHalfRows / 16;  // blocks of 16 rows of a draining thread
   extern __shared__ uint8_t smem_raw[];
   uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   __shared__ uint64_t s_full[kMaxStages], s_empty[kMaxStages], s_afull[kMaxA], s_afree[kMaxA], s_dfull[2], s_dfree[2],
@@ -272,8 +288,8 @@ __global__ void __launch_bounds__(Shape<kWide>::kThreads, Shape<kWide>::kPerSm)
     tma_prefetch_desc(&tm_w);
     tma_prefetch_desc(&tm_x);
     for (int s = 0; s < S::kStages; ++s) {
-      mbar_init(&s_full[s], 1);
-      mbar_init(&s_empty[s], 9);  // eight unpacking warps and the MMAs
+      mbar_init(&s_full[s], 33);                   // the leader's copies, every lane's pairs
+      mbar_init(&s_empty[s], 9 + 4 * S::kHalves);  // eight unpacking warps, the draining ones and the MMAs
     }
     for (int s = 0; s < S::kA; ++s) {
       mbar_init(&s_afull[s], 8);
@@ -302,8 +318,6 @@ __global__ void __launch_bounds__(Shape<kWide>::kThreads, Shape<kWide>::kPerSm)
   const int u1 = static_cast<int>(static_cast<int64_t>(units) * (rank + 1) / split);
   const int t = (warp & 3) * 32 + lane;                       // output of the unpacking and draining threads
   const uint32_t tlane = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
-  const uint32_t *pair = p.pairs + static_cast<int64_t>(min(o0 + t, p.N - 1)) * groups;
-  const bool whole = groups % U == 0;
   const int half_rows = kWide ? (n / 16 + 1) / 2 * 16 : n;    // rows of the first draining half
   const int r_lo = kWide && warp >= S::kWarpDrain + 4 ? half_rows : 0;  // this thread's first row (draining)
   const int my_rows = min(half_rows, n - r_lo);
@@ -322,6 +336,25 @@ __global__ void __launch_bounds__(Shape<kWide>::kThreads, Shape<kWide>::kPerSm)
       ok = __all_sync(0xffffffffu, mbar_wait_lean(&s_empty[st], ((issued / S::kStages) & 1) ^ 1, &s_abort));
       if (!ok) break;
       uint8_t *stage = smem + st * S::kStage;
+      // Pairs: four outputs per lane, by asynchronous copies that arrive on the stage's barrier
+      // themselves.  (Loads into registers ahead of time do not work here: a warp's arrivals
+      // release, and so wait for every load that it has in flight.  They cost 1300 cycles a unit.)
+#pragma unroll
+      for (int r = lane; r < kOut; r += 32) {
+        const uint32_t *from = p.pairs + static_cast<int64_t>(min(o0 + r, p.N - 1)) * groups + u * U;
+        const uint32_t to = smem_u32(stage + kCodes + S::kX) + r * (U * 4);
+        if (groups % U == 0) {
+          asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(from), "n"(U * 4) : "memory");
+        } else {
+#pragma unroll
+          for (int q = 0; q < U; ++q) {
+            const bool in = u * U + q < groups;  // (zeros past the last group)
+            asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to + q * 4), "l"(in ? from + q : p.pairs),
+                         "r"(in ? 4u : 0u) : "memory");
+          }
+        }
+      }
+      asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&s_full[st])) : "memory");
       if (leader) {
         mbar_arrive_expect_tx(&s_full[st], kCodes + n * 256);
         tma_load_2d(stage, &tm_w, u * (kUnit / 2), o0, &s_full[st], pol_w);
@@ -329,6 +362,7 @@ __global__ void __launch_bounds__(Shape<kWide>::kThreads, Shape<kWide>::kPerSm)
         tma_load_2d(stage + kCodes + S::kX / 2, &tm_x, u * kUnit + 64, n0, &s_full[st], pol);
       }
     }
+    asm volatile("cp.async.wait_all;" ::: "memory");
     if (!ok && leader)  // every copy issued must land before the CTA's shared memory goes away
       for (uint32_t j = issued > S::kStages ? issued - S::kStages : 0; j < issued; ++j)
         mbar_wait_unabortable(&s_full[j % S::kStages], (j / S::kStages) & 1);
@@ -337,7 +371,7 @@ __global__ void __launch_bounds__(Shape<kWide>::kThreads, Shape<kWide>::kPerSm)
     const uint32_t idesc = idesc_bf16_f32(kOut, n);
     const bool leader = elect_one();
     const uint32_t base = smem_u32(smem);
-    uint32_t it = 0, gi = 0;
+    uint32_t it = 0, bi = 0;
     auto wait = [&](uint64_t *bar, uint32_t parity) {
       ok = __all_sync(0xffffffffu, mbar_wait_lean(bar, parity, &s_abort)) && ok;
     };
@@ -349,20 +383,23 @@ __global__ void __launch_bounds__(Shape<kWide>::kThreads, Shape<kWide>::kPerSm)
       const uint64_t dx = smem_desc_sw128(base + st * S::kStage + kCodes);
       const int ng = min(U, groups - u * U);
 #pragma unroll
-      for (int q = 0; q < U; ++q) {
-        if (q >= ng) break;
-        const int db = gi & 1;
-        wait(&s_dfree[db], ((gi / 2) & 1) ^ 1);
+      for (int q0 = 0; q0 < U; q0 += S::kBlock) {
+        if (q0 >= ng) break;
+        const int db = bi & 1;
+        wait(&s_dfree[db], ((bi / 2) & 1) ^ 1);
         tc_fence_after();
 #pragma unroll
-        for (int k = 0; k < G / 16; ++k) {
-          const int kk = q * (G / 16) + k;  // four per 64-k slab
-          const uint32_t off = ((kk / 4) * (S::kX / 2) + (kk % 4) * 32) >> 4;
-          if (leader)
-            tc_mma_f16_ta(tmem + S::kColD + db * S::kRows, tmem + S::kColA + as * 64 + kk * 8, dx + off, idesc, k > 0);
+        for (int q = q0; q < q0 + S::kBlock; ++q) {  // (a group past the last: zeros)
+          const uint32_t d = tmem + S::kColD + (db * S::kBlock + q - q0) * S::kRows;
+#pragma unroll
+          for (int k = 0; k < G / 16; ++k) {
+            const int kk = q * (G / 16) + k;  // four per 64-k slab
+            const uint32_t off = ((kk / 4) * (S::kX / 2) + (kk % 4) * 32) >> 4;
+            if (leader) tc_mma_f16_ta(d, tmem + S::kColA + as * 64 + kk * 8, dx + off, idesc, k > 0);
+          }
         }
         if (leader) tc_commit(&s_dfull[db]);
-        ++gi;
+        ++bi;
       }
       if (leader) {
         tc_commit(&s_afree[as]);
@@ -377,17 +414,16 @@ __global__ void __launch_bounds__(Shape<kWide>::kThreads, Shape<kWide>::kPerSm)
   } else if (warp >= S::kWarpUnpack) {
     // ---- unpacking: two threads per output, 64 k each ----
     const int part = (warp - S::kWarpUnpack) / 4;
-    uint32_t pr[2][U];
-    if (u0 < u1) load_unit_pairs<U>(pair, u0, groups, whole, pr[0]);
     uint32_t it = 0;
-    auto unit = [&](int u, const uint32_t (&now)[U], uint32_t (&next)[U]) {
-      if (u + 1 < u1) load_unit_pairs<U>(pair, u + 1, groups, whole, next);
+    for (int u = u0; u < u1; ++u, ++it) {
       const int st = it % S::kStages, as = it % S::kA;
       ok = mbar_wait_lean(&s_full[st], (it / S::kStages) & 1, &s_abort) &&
            mbar_wait_lean(&s_afree[as], ((it / S::kA) & 1) ^ 1, &s_abort);
       ok = __all_sync(0xffffffffu, ok);
-      if (!ok) return;
+      if (!ok) break;
       tc_fence_after();
+      uint32_t now[U];
+      read_pairs<U>(smem + st * S::kStage + kCodes + S::kX, t, now);
       const uint8_t *row = smem + st * S::kStage + t * 64;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -409,52 +445,51 @@ __global__ void __launch_bounds__(Shape<kWide>::kThreads, Shape<kWide>::kPerSm)
         mbar_arrive(&s_afull[as]);
         mbar_arrive(&s_empty[st]);
       }
-      ++it;
-    };
-    for (int u = u0; ok && u < u1; u += 2) {
-      unit(u, pr[0], pr[1]);
-      if (ok && u + 1 < u1) unit(u + 1, pr[1], pr[0]);
     }
   } else {
     // ---- draining: a group's sums under the outputs' scales ----
-    uint32_t pr[2][U];
-    if (u0 < u1) load_unit_pairs<U>(pair, u0, groups, whole, pr[0]);
 #pragma unroll
     for (int r = 0; r < S::kHalfRows / 2; ++r) sum[r] = f2(0.f, 0.f);
-    uint32_t gi = 0;
-    auto unit = [&](int u, const uint32_t (&now)[U], uint32_t (&next)[U]) {
-      if (u + 1 < u1) load_unit_pairs<U>(pair, u + 1, groups, whole, next);
-      const int ng = min(U, groups - u * U);
+    uint32_t it = 0, bi = 0;
+    for (int u = u0; ok && u < u1; ++u, ++it) {
+      const int ng = min(U, groups - u * U), st = it % S::kStages;
+      uint32_t now[U];
 #pragma unroll
-      for (int q = 0; q < U; ++q) {
-        if (q >= ng) break;
-        const int db = gi & 1;
-        ok = __all_sync(0xffffffffu, mbar_wait_lean(&s_dfull[db], (gi / 2) & 1, &s_abort));
-        if (!ok) return;
+      for (int q0 = 0; q0 < U; q0 += S::kBlock) {
+        if (q0 >= ng) break;
+        const int db = bi & 1;
+        // (The sums come after their unit's copies; the first wait is for the reads of those.)
+        if (q0 == 0) ok = mbar_wait_lean(&s_full[st], (it / S::kStages) & 1, &s_abort);
+        ok = __all_sync(0xffffffffu, ok && mbar_wait_lean(&s_dfull[db], (bi / 2) & 1, &s_abort));
+        if (!ok) break;
         tc_fence_after();
-        const float s = int4::pair_of(now[q]).x;
-        const F2 ss = f2(s, s);
-        const uint32_t from = tlane + S::kColD + db * S::kRows + r_lo;
+        if (q0 == 0) read_pairs<U>(smem + st * S::kStage + kCodes + S::kX, t, now);
 #pragma unroll
-        for (int k = 0; k < kBlocks; ++k) {
-          if (k * 16 >= my_rows) break;
-          uint32_t y[16];
-          tmem_ld8(from + k * 16, y);
-          tmem_ld8(from + k * 16 + 8, y + 8);
-          tmem_wait_ld();
+        for (int q = q0; q < q0 + S::kBlock; ++q) {
+          if (q >= ng) break;
+          const float s = int4::pair_of(now[q]).x;
+          const F2 ss = f2(s, s);
+          const uint32_t from = tlane + S::kColD + (db * S::kBlock + q - q0) * S::kRows + r_lo;
 #pragma unroll
-          for (int e = 0; e < 16; e += 2)
-            sum[k * 8 + e / 2] = f2_fma(f2(__uint_as_float(y[e]), __uint_as_float(y[e + 1])), ss, sum[k * 8 + e / 2]);
+          for (int k = 0; k < S::kHalfRows; k += 32) {
+            if (k >= my_rows) break;
+            uint32_t y[32];
+#pragma unroll
+            for (int j = 0; j < 32; j += 8) tmem_ld8(from + k + j, y + j);  // (columns past the tile's rows: unused)
+            tmem_wait_ld();
+#pragma unroll
+            for (int e = 0; e < 32; e += 2)
+              sum[(k + e) / 2] = f2_fma(f2(__uint_as_float(y[e]), __uint_as_float(y[e + 1])), ss, sum[(k + e) / 2]);
+          }
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&s_dfree[db]);
-        ++gi;
+        if (lane == 0) {
+          mbar_arrive(&s_dfree[db]);
+          if (q0 == 0) mbar_arrive(&s_empty[st]);
+        }
+        ++bi;
       }
-    };
-    for (int u = u0; ok && u < u1; u += 2) {
-      unit(u, pr[0], pr[1]);
-      if (ok && u + 1 < u1) unit(u + 1, pr[1], pr[0]);
     }
   }
   if (!ok && lane == 0) atomicOr(p.status, SPADE_DEV_TIMEOUT);
@@ -558,7 +593,7 @@ static cudaError_t few_rows(const Params &p, const CUtensorMap &tm, bool wide, c
 
 template <int G, bool kWide>
 static cudaError_t rows(const Params &p, const CUtensorMap &w, const CUtensorMap &x, cudaStream_t s) {
-  using S = tc::Shape<kWide>;
+  using S = tc::Shape<G, kWide>;
   static OncePerDevice once;
   const cudaError_t e = set_max_smem(once, S::kBytes, tc::rows_kernel<G, kWide>);
   if (e != cudaSuccess) return e;
@@ -619,8 +654,8 @@ extern "C" spade_status spade_linear_w4(const void *x, const void *codes, const 
         : group == 64 ? w4::few_rows<64>(p, w, wide, s)
                       : w4::few_rows<32>(p, w, wide, s);
   } else {
-    const bool wide = R > w4::tc::Shape<false>::kRows;
-    const int most = wide ? w4::tc::Shape<true>::kRows : w4::tc::Shape<false>::kRows;
+    const bool wide = R > w4::tc::kNarrow;
+    const int most = wide ? w4::tc::kMost : w4::tc::kNarrow;
     const int row_tiles = (R - 1) / most + 1;
     if (row_tiles > 65535) return fail(SPADE_ERR_SHAPE, "spade_linear_w4: R = %d exceeds %d rows per call", R, 65535 * most);
     p.tile_rows = (R - 1) / row_tiles + 1;

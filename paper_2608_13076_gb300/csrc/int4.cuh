@@ -59,7 +59,7 @@ struct Cache {
   // Pool row of head 0 of sequence b's slot, in rows of D / 2 code bytes (head h is
   // h * page_size rows on); negative where the page is not in the pool.
   __device__ int64_t row(int b, int slot) const {
-    const int page = __ldg(block_table + static_cast<int64_t>(b) * max_pages + slot / page_size);
+    const int page = block_table[static_cast<int64_t>(b) * max_pages + slot / page_size];
     if (page < 0 || page >= num_pages) return -1;
     return static_cast<int64_t>(page) * Hkv * page_size + slot % page_size;
   }

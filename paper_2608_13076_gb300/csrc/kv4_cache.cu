@@ -10,6 +10,7 @@
 
 #include "int4.cuh"
 #include "internal.h"
+#include "launch.h"
 #include "ptx.cuh"
 
 namespace spade {
@@ -53,9 +54,16 @@ SPADE_DEVICE int block_error(const NormRope &p, int ctx, int k, int q0, int q1) 
   return end > p.max_pos ? SPADE_DEV_BAD_INDEX : 0;
 }
 
-// Group of 64 dims (eight lanes) into the cache: the lane's code word, and the pair
-// by the group's first lane.  Every operation is one IEEE fp32 operation.
-SPADE_DEVICE void store_group(const float (&x)[8], uint32_t *codes, uint32_t *pair, bool first) {
+// x / s for a scale s, correctly rounded: with y = 1 / s correctly rounded and q = x y,
+// q + (x - q s) y is (Markstein, IBM J. Res. Dev. 34, 1990; the significand of s, a
+// float16, is not all ones).  Three operations for a division's dozen.
+SPADE_DEVICE float divided(float x, float s, float y) {
+  const float q = __fmul_rn(x, y);
+  return __fmaf_rn(__fmaf_rn(-q, s, x), y, q);
+}
+
+// Group of 64 dims (eight lanes): the lane's code word and the group's pair.
+SPADE_DEVICE void quantise(const float (&x)[8], uint32_t &codes, uint32_t &pair) {
   float lo = 0.f, hi = 0.f;
   bool finite = true;
 #pragma unroll
@@ -68,29 +76,34 @@ SPADE_DEVICE void store_group(const float (&x)[8], uint32_t *codes, uint32_t *pa
   for (int o = 1; o < 8; o *= 2) {
     lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
     hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-    finite = __shfl_xor_sync(0xffffffffu, static_cast<int>(finite), o) && finite;
   }
+  const unsigned vote = __ballot_sync(0xffffffffu, finite) >> (threadIdx.x & 24) & 0xffu;
   // (hi - lo overflows for spans past fp32's range: infinity, cut like any other.)
   const __half hs = __float2half_rn(fminf(__fmul_rn(__fsub_rn(hi, lo), 1.f / 15.f), int4::kMaxScale));
   const float s = __half2float(hs);
-  const bool real = finite && s > 0.f;
-  const float z = real ? fminf(rintf(__fdiv_rn(-lo, s)), 15.f) : 0.f;
+  const bool real = vote == 0xffu && s > 0.f;
+  const float y = __frcp_rn(real ? s : 1.f);
+  constexpr float kWhole = 12582912.f;  // 1.5 2^23: adding it rounds to a whole number, ties to even
+  const float z = real ? fminf(divided(-lo, s, y) + kWhole - kWhole, 15.f) : 0.f;
   uint32_t w = 0;
-  if (real) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float c = fminf(fmaxf(rintf(__fdiv_rn(x[e], s)) + z, 0.f), 15.f);
-      w |= static_cast<uint32_t>(c) << (4 * ((e >> 1) + 4 * (e & 1)));
-    }
+  for (int e = 0; e < 8; ++e) {
+    // (A scale that was cut leaves quotients of any size.)
+    const float q = fminf(fmaxf(divided(x[e], s, y), -64.f), 64.f);
+    const int c = __float_as_int(q + kWhole) - __float_as_int(kWhole) + static_cast<int>(z);
+    w |= static_cast<uint32_t>(min(max(c, 0), 15)) << (4 * ((e >> 1) + 4 * (e & 1)));
   }
-  *codes = w;
-  if (first) {
-    const __half2 h = __halves2half2(finite ? hs : __ushort_as_half(0x7fff), __float2half_rn(z));
-    *pair = *reinterpret_cast<const uint32_t *>(&h);
-  }
+  codes = real ? w : 0u;
+  const __half2 h = __halves2half2(vote == 0xffu ? hs : __ushort_as_half(0x7fff), __float2half_rn(z));
+  pair = *reinterpret_cast<const uint32_t *>(&h);
 }
 
-template <int D>
+// A warp takes kHeads x 32 / (D / 8) heads of one row, all their loads in flight at once;
+// the rotation's angles, the same for every head, stay in registers.  Bound by the bytes:
+// a row's heads once in, the queries out in bf16 and the rest in 4 bits.  (One group of
+// heads per warp, a quantisation of every head, queries too, and a division per number:
+// 12288 rows took 204 us.)
+template <int D, int kHeads>
 __global__ void __launch_bounds__(kThreads) norm_rope_kernel(const __grid_constant__ NormRope p) {
   constexpr int kLanes = D / 8;          // lanes of a head
   constexpr int kSlots = 32 / kLanes;    // heads side by side in a warp
@@ -98,6 +111,8 @@ __global__ void __launch_bounds__(kThreads) norm_rope_kernel(const __grid_consta
   const int lane = threadIdx.x & 31;
   const int item = blockIdx.x * kWarps + (threadIdx.x >> 5);
   const int i = item / p.parts, part = item - i * p.parts;
+  griddep_wait();
+  griddep_launch_dependents();
   const int ctx = p.ctx_lens[b], k = p.n_draft[b], q0 = p.cu_q[b], q1 = p.cu_q[b + 1];
   const int err = block_error(p, ctx, k, q0, q1);
   if (err) {
@@ -109,55 +124,64 @@ __global__ void __launch_bounds__(kThreads) norm_rope_kernel(const __grid_consta
   const int row = q0 + i;
   const int sub = lane / kLanes, l = lane % kLanes;
   const int Hkv = p.cache.Hkv, heads = p.Hq + 2 * Hkv;
-  // cos and sin of the lane's eight dims (the second half of the dims repeats the first's).
+  const int h0 = part * kSlots * kHeads + sub;
+  const uint4 *src = reinterpret_cast<const uint4 *>(p.qkv) + static_cast<int64_t>(row) * heads * kLanes + l;
+  uint4 in[kHeads];
+#pragma unroll
+  for (int j = 0; j < kHeads; ++j) {
+    const int h = h0 + j * kSlots;
+    in[j] = h < heads ? src[h * kLanes] : make_uint4(0, 0, 0, 0);
+  }
+  // cos and sin of the lane's eight dims (the second half of the dims repeats the first's): a
+  // dim of the first half becomes own cos - other sin, one of the second own cos + other sin,
+  // so the sine carries the sign.
+  const bool second = l >= kLanes / 2;
   float cs[8], sn[8];
   const float4 *turn = p.rope + (static_cast<int64_t>(pos) * (D / 2) + (l % (kLanes / 2)) * 8) / 2;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    const float4 t = __ldg(turn + e);
+    const float4 t = turn[e];
     cs[2 * e] = t.x;
-    sn[2 * e] = t.y;
+    sn[2 * e] = second ? t.y : -t.y;
     cs[2 * e + 1] = t.z;
-    sn[2 * e + 1] = t.w;
+    sn[2 * e + 1] = second ? t.w : -t.w;
   }
-  const int64_t slot = p.cache.row(b, pos);
-  if (slot < 0 && part == 0 && lane == 0) atomicOr(p.status, SPADE_DEV_BAD_INDEX);
-  const bool second = l >= kLanes / 2;
-  const uint4 *src = reinterpret_cast<const uint4 *>(p.qkv) + static_cast<int64_t>(row) * heads * kLanes + l;
-  for (int h0 = part * kSlots; h0 < heads; h0 += p.parts * kSlots) {
-    const int h = h0 + sub;
-    const bool in = h < heads;
+  const bool stores = (part + 1) * kSlots * kHeads > p.Hq;  // the warp has key or value heads
+  const int64_t slot = stores ? p.cache.row(b, pos) : 0;
+  if (slot < 0 && lane == 0) atomicOr(p.status, SPADE_DEV_BAD_INDEX);
+#pragma unroll
+  for (int j = 0; j < kHeads; ++j) {
+    const int h = h0 + j * kSlots;
+    if (h - sub >= heads) break;
     float x[8];
-    unpack8(in ? __ldg(src + h * kLanes) : make_uint4(0, 0, 0, 0), x);
+    unpack8(in[j], x);
     const bool is_q = h < p.Hq, is_v = h >= p.Hq + Hkv;
-    const __nv_bfloat16 *weight = is_q ? p.q_norm : p.k_norm;
-    // (the shuffles are the whole warp's: heads of both kinds may share it)
-    float sum = 0.f;
+    // (The shuffles are the whole warp's, whatever its heads are.)
+    if (!__all_sync(0xffffffffu, is_v)) {
+      const __nv_bfloat16 *weight = is_q ? p.q_norm : p.k_norm;
+      float sum = 0.f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) sum = fmaf(x[e], x[e], sum);
+      for (int e = 0; e < 8; ++e) sum = fmaf(x[e], x[e], sum);
 #pragma unroll
-    for (int o = 1; o < kLanes; o *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if (!is_v && weight) {
-      const float r = rsqrtf(__fadd_rn(sum * (1.f / D), p.eps));
-      float w[8];
-      unpack8(__ldg(reinterpret_cast<const uint4 *>(weight) + l), w);
+      for (int o = 1; o < kLanes; o *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+      if (!is_v && weight) {
+        const float r = rsqrtf(__fadd_rn(sum * (1.f / D), p.eps));
+        float w[8];
+        unpack8(reinterpret_cast<const uint4 *>(weight)[l], w);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = __fmul_rn(__fmul_rn(x[e], r), w[e]);
-    }
+        for (int e = 0; e < 8; ++e) x[e] = __fmul_rn(__fmul_rn(x[e], r), w[e]);
+      }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float other = __shfl_xor_sync(0xffffffffu, x[e], kLanes / 2);
-      if (!is_v) {
-        const float turned = __fmul_rn(other, sn[e]), own = __fmul_rn(x[e], cs[e]);
-        x[e] = second ? __fadd_rn(own, turned) : __fsub_rn(own, turned);
+      for (int e = 0; e < 8; ++e) {
+        const float other = __shfl_xor_sync(0xffffffffu, x[e], kLanes / 2);
+        if (!is_v) x[e] = __fadd_rn(__fmul_rn(x[e], cs[e]), __fmul_rn(other, sn[e]));
       }
     }
-    if (in && is_q) {
-      reinterpret_cast<uint4 *>(p.q_out)[(static_cast<int64_t>(row) * p.Hq + h) * kLanes + l] = pack8(x);
-    }
-    uint32_t code = 0, pair = 0;
-    store_group(x, &code, &pair, true);
-    if (in && !is_q && slot >= 0) {
+    if (is_q) reinterpret_cast<uint4 *>(p.q_out)[(static_cast<int64_t>(row) * p.Hq + h) * kLanes + l] = pack8(x);
+    if (__all_sync(0xffffffffu, is_q)) continue;
+    uint32_t code, pair;
+    quantise(x, code, pair);
+    if (h < heads && !is_q && slot >= 0) {
       const int64_t r = slot + static_cast<int64_t>(h - p.Hq - (is_v ? Hkv : 0)) * p.cache.page_size;
       reinterpret_cast<uint32_t *>(is_v ? p.cache.v_codes : p.cache.k_codes)[r * kLanes + l] = code;
       if (l % 8 == 0) (is_v ? p.cache.v_params : p.cache.k_params)[r * (D / int4::kKvGroup) + l / 8] = pair;
@@ -172,6 +196,8 @@ __global__ void __launch_bounds__(kThreads) commit_kernel(const __grid_constant_
                                                          const int32_t *accepted, const int32_t *n_draft,
                                                          int32_t *new_ctx_lens, int32_t *status) {
   const int b = blockIdx.x;
+  griddep_wait();
+  griddep_launch_dependents();
   const int ctx = ctx_lens[b], a = accepted[b], k = n_draft[b];
   int bad = 0;
   if (ctx < 0 || k < 0 || a < 0 || a > k) bad = SPADE_DEV_BAD_INDEX;
@@ -186,27 +212,36 @@ __global__ void __launch_bounds__(kThreads) commit_kernel(const __grid_constant_
     if (bad) atomicOr(status, bad);
   }
   if (bad) return;
-  const int words = c.D / 8, pairs = c.D / int4::kKvGroup;  // of a head's slot
-  const int per = words + pairs;
-  for (int64_t e = threadIdx.x; e < static_cast<int64_t>(n) * c.Hkv * per; e += kThreads) {
-    const int j = static_cast<int>(e % per);
-    const int64_t r = e / per;
-    const int64_t at = c.row(b, lo + static_cast<int>(r / c.Hkv)) + static_cast<int64_t>(r % c.Hkv) * c.page_size;
-    if (j < words) {
-      reinterpret_cast<uint32_t *>(c.k_codes)[at * words + j] = 0;
-      reinterpret_cast<uint32_t *>(c.v_codes)[at * words + j] = 0;
-    } else {
-      c.k_params[at * pairs + j - words] = 0;
-      c.v_params[at * pairs + j - words] = 0;
+  // A warp per slot: its heads' code words and pairs.
+  const int words = c.D / 8, pairs = c.D / int4::kKvGroup, per = words + pairs;
+  const int lane = threadIdx.x & 31;
+  for (int s = threadIdx.x >> 5; s < n; s += kWarps) {
+    const int64_t slot = c.row(b, lo + s);
+    for (int e = lane; e < c.Hkv * per; e += 32) {
+      const int h = e / per, j = e - h * per;
+      const int64_t at = slot + static_cast<int64_t>(h) * c.page_size;
+      if (j < words) {
+        reinterpret_cast<uint32_t *>(c.k_codes)[at * words + j] = 0;
+        reinterpret_cast<uint32_t *>(c.v_codes)[at * words + j] = 0;
+      } else {
+        c.k_params[at * pairs + j - words] = 0;
+        c.v_params[at * pairs + j - words] = 0;
+      }
     }
   }
 }
 
 // ---- read ----------------------------------------------------------------------------------
+// Warps stride the slots: warp w takes part w % parts (32 / (D / 8) heads of keys and
+// values) of slots w / parts, + step, ...
+template <int D>
 __global__ void __launch_bounds__(kThreads) read_kernel(const __grid_constant__ Cache c, const int32_t *starts,
                                                        const int32_t *cu_rows, uint4 *k_out, uint4 *v_out, int R,
-                                                       int32_t *status) {
+                                                       int parts, int32_t *status) {
+  constexpr int kLanes = D / 8;
   const int b = blockIdx.y;
+  griddep_wait();
+  griddep_launch_dependents();
   const int s0 = starts[b], r0 = cu_rows[b], r1 = cu_rows[b + 1];
   int bad = 0;
   if (s0 < 0 || r0 < 0 || r1 < r0 || r1 > R) bad = SPADE_DEV_BAD_INDEX;
@@ -215,25 +250,28 @@ __global__ void __launch_bounds__(kThreads) read_kernel(const __grid_constant__ 
     if (blockIdx.x == 0 && threadIdx.x == 0) atomicOr(status, bad);
     return;
   }
-  const int words = c.D / 8;
-  const int per = c.Hkv * words;  // words of a slot
-  for (int64_t e = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; e < static_cast<int64_t>(r1 - r0) * per;
-       e += static_cast<int64_t>(gridDim.x) * kThreads) {
-    const int i = static_cast<int>(e / per), j = static_cast<int>(e % per);
-    const int h = j / words, l = j % words;
-    const int64_t slot = c.row(b, s0 + i);
-    if (slot < 0 && j == 0) atomicOr(status, SPADE_DEV_BAD_INDEX);
+  const int lane = threadIdx.x & 31, w = blockIdx.x * kWarps + (threadIdx.x >> 5);
+  const int part = w % parts, step = gridDim.x * kWarps / parts;
+  const int h = part * (32 / kLanes) + lane / kLanes, l = lane % kLanes;
+  for (int64_t i = w / parts; i < r1 - r0; i += step) {
+    const int64_t slot = c.row(b, s0 + static_cast<int>(i));
+    if (slot < 0 && part == 0 && lane == 0) atomicOr(status, SPADE_DEV_BAD_INDEX);
+    if (h >= c.Hkv) continue;
     const int64_t at = slot + static_cast<int64_t>(h) * c.page_size;
+    uint32_t word[2] = {}, pair[2] = {};
+    if (slot >= 0) {
+      word[0] = reinterpret_cast<const uint32_t *>(c.k_codes)[at * kLanes + l];
+      word[1] = reinterpret_cast<const uint32_t *>(c.v_codes)[at * kLanes + l];
+      pair[0] = c.k_params[at * (D / int4::kKvGroup) + l / 8];
+      pair[1] = c.v_params[at * (D / int4::kKvGroup) + l / 8];
+    }
 #pragma unroll
     for (int kv = 0; kv < 2; ++kv) {
-      float x[8] = {};
-      if (slot >= 0) {
-        const uint32_t w = __ldg(reinterpret_cast<const uint32_t *>(kv ? c.v_codes : c.k_codes) + at * words + l);
-        const float2 pair = int4::pair_of(__ldg((kv ? c.v_params : c.k_params) + at * (words / 8) + l / 8));
+      const float2 p = int4::pair_of(pair[kv]);
+      float x[8];
 #pragma unroll
-        for (int e8 = 0; e8 < 8; ++e8) x[e8] = pair.x * (static_cast<float>(int4::code_of(w, e8)) - pair.y);
-      }
-      (kv ? v_out : k_out)[static_cast<int64_t>(r0) * per + e] = pack8(x);
+      for (int e = 0; e < 8; ++e) x[e] = p.x * (static_cast<float>(int4::code_of(word[kv], e)) - p.y);
+      (kv ? v_out : k_out)[((r0 + i) * c.Hkv + h) * kLanes + l] = pack8(x);
     }
   }
 }
@@ -301,17 +339,19 @@ extern "C" spade_status spade_verify_qk_norm_rope_kv4(
   p.q_out = static_cast<__nv_bfloat16 *>(q_out);
   p.ctx_lens = ctx_lens; p.n_draft = n_draft; p.cu_q = cu_q; p.status = status;
   p.R = R; p.Hq = Hq; p.max_pos = max_pos; p.max_k = max_k; p.eps = eps;
-  const int slots = 256 / D;
-  p.parts = (Hq + 2 * Hkv + slots - 1) / slots;
+  // Heads of a warp: one group of them while the rows are few (latency), four when the
+  // warps fill the GPU either way.
+  const int slots = 256 / D, heads = Hq + 2 * Hkv;
+  const bool many = static_cast<int64_t>(R) * heads / (4 * slots) >= 16 * static_cast<int64_t>(sms);
+  p.parts = (heads + slots * (many ? 4 : 1) - 1) / (slots * (many ? 4 : 1));
   // A block longer than the rows given cannot be valid.
   const int64_t longest = (max_k < R ? max_k : R - 1) + int64_t(1);
   const int64_t items = longest * p.parts;
   if (items > (int64_t(1) << 31) - kv4::kWarps) return fail(SPADE_ERR_CAPACITY, "%s: too many rows per sequence", name);
   const dim3 grid(static_cast<unsigned>((items + kv4::kWarps - 1) / kv4::kWarps), B);
-  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  if (D == 64) kv4::norm_rope_kernel<64><<<grid, kv4::kThreads, 0, s>>>(p);
-  else kv4::norm_rope_kernel<128><<<grid, kv4::kThreads, 0, s>>>(p);
-  const cudaError_t e = cudaGetLastError();
+  auto kern = D == 64 ? (many ? kv4::norm_rope_kernel<64, 4> : kv4::norm_rope_kernel<64, 1>)
+                      : (many ? kv4::norm_rope_kernel<128, 4> : kv4::norm_rope_kernel<128, 1>);
+  const cudaError_t e = launch(kern, grid, 1, kv4::kThreads, 0, reinterpret_cast<cudaStream_t>(stream), p);
   return e == cudaSuccess ? SPADE_OK : cuda_fail(e, "verify_qk_norm_rope_kv4 launch");
 }
 
@@ -330,9 +370,8 @@ extern "C" spade_status spade_kv_commit_kv4(void *k_codes, void *k_params, void 
   if (st != SPADE_OK) return st;
   st = device_info(nullptr, nullptr);
   if (st != SPADE_OK) return st;
-  kv4::commit_kernel<<<B, kv4::kThreads, 0, reinterpret_cast<cudaStream_t>(stream)>>>(
-      c, ctx_lens, accepted_len, n_draft, new_ctx_lens, status);
-  const cudaError_t e = cudaGetLastError();
+  const cudaError_t e = launch(kv4::commit_kernel, dim3(B), 1, kv4::kThreads, 0, reinterpret_cast<cudaStream_t>(stream), c,
+                               ctx_lens, accepted_len, n_draft, new_ctx_lens, status);
   return e == cudaSuccess ? SPADE_OK : cuda_fail(e, "kv_commit_kv4 launch");
 }
 
@@ -354,13 +393,17 @@ extern "C" spade_status spade_kv_read_kv4(const void *k_codes, const void *k_par
   int sms = 0;
   st = device_info(&sms, nullptr);
   if (st != SPADE_OK) return st;
-  // Enough CTAs for the rows if one sequence has them all, but no more than fill the
-  // GPU a few times over: the rest is the loop's.
-  const int64_t all = (static_cast<int64_t>(R) * Hkv * (D / 8) + kv4::kThreads - 1) / kv4::kThreads;
-  const int64_t most = (16 * static_cast<int64_t>(sms) + B - 1) / B;
-  const dim3 grid(static_cast<unsigned>(all < most ? all : most), B);
-  kv4::read_kernel<<<grid, kv4::kThreads, 0, reinterpret_cast<cudaStream_t>(stream)>>>(
-      c, starts, cu_rows, static_cast<uint4 *>(k_out), static_cast<uint4 *>(v_out), R, status);
-  const cudaError_t e = cudaGetLastError();
+  // Enough warps for the rows if one sequence has them all, but no more than fill the GPU
+  // a few times over: the rest is the loop's.  (Whole rounds of `parts`, so that a warp
+  // keeps its part.)
+  const int parts = (Hkv * (D / 8) + 31) / 32;
+  const int64_t most = (16 * static_cast<int64_t>(sms) + B - 1) / B;       // CTAs per sequence
+  const int64_t rows = most * kv4::kWarps / parts + 1;                     // rows that those take at once
+  const int64_t warps = (R < rows ? R : rows) * parts;
+  const unsigned round = parts % kv4::kWarps ? parts : parts / kv4::kWarps;  // CTAs of whole rounds
+  const unsigned ctas = static_cast<unsigned>((warps + kv4::kWarps - 1) / kv4::kWarps + round - 1) / round * round;
+  const cudaError_t e = launch(D == 64 ? kv4::read_kernel<64> : kv4::read_kernel<128>, dim3(ctas, B), 1, kv4::kThreads, 0,
+                               reinterpret_cast<cudaStream_t>(stream), c, starts, cu_rows, static_cast<uint4 *>(k_out),
+                               static_cast<uint4 *>(v_out), R, parts, status);
   return e == cudaSuccess ? SPADE_OK : cuda_fail(e, "kv_read_kv4 launch");
 }

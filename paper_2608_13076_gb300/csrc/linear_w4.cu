@@ -5,6 +5,7 @@
 
 #include "int4.cuh"
 #include "internal.h"
+#include "launch.h"
 #include "ptx.cuh"
 
 namespace spade {
@@ -71,19 +72,19 @@ SPADE_DEVICE void load_unit_pairs(const uint32_t *pairs, int u, int groups, bool
   const uint32_t *at = pairs + static_cast<int64_t>(u) * U;
   if constexpr (U == 4) {
     if (whole) {
-      const uint4 v = __ldg(reinterpret_cast<const uint4 *>(at));
+      const uint4 v = *reinterpret_cast<const uint4 *>(at);
       p[0] = v.x; p[1] = v.y; p[2] = v.z; p[3] = v.w;
       return;
     }
   } else if constexpr (U == 2) {
     if (whole) {
-      const uint2 v = __ldg(reinterpret_cast<const uint2 *>(at));
+      const uint2 v = *reinterpret_cast<const uint2 *>(at);
       p[0] = v.x; p[1] = v.y;
       return;
     }
   }
 #pragma unroll
-  for (int q = 0; q < U; ++q) p[q] = u * U + q < groups ? __ldg(at + q) : 0u;
+  for (int q = 0; q < U; ++q) p[q] = u * U + q < groups ? at[q] : 0u;
 }
 
 template <int G, int MT>
@@ -144,7 +145,7 @@ __global__ void __launch_bounds__(kThreads) few_rows_kernel(const __grid_constan
     for (int q = 0; q < U; ++q)
 #pragma unroll
       for (int e = 0; e < W; ++e)
-        a.xv[q * W + e] = u * U + q < groups ? __ldg(x + (u * U + q) * (G / 8) + e) : make_uint4(0, 0, 0, 0);
+        a.xv[q * W + e] = u * U + q < groups ? x[(u * U + q) * (G / 8) + e] : make_uint4(0, 0, 0, 0);
   };
   if (mine) load_rest(warp, rest[0]);
   float acc[MT][4] = {};
@@ -554,26 +555,6 @@ __global__ void __launch_bounds__(Shape<G, kWide>::kThreads, Shape<G, kWide>::kP
 }
 
 }  // namespace tc
-
-// `grid` CTAs of `kern` in clusters of `cluster`, programmatic dependent launch.
-template <class... A>
-static cudaError_t launch(void (*kern)(A...), dim3 grid, unsigned cluster, unsigned threads, size_t smem, cudaStream_t s,
-                          A... a) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid;
-  cfg.blockDim = dim3(threads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = s;
-  cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = cluster;
-  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = cluster > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, kern, a...);
-}
 
 template <int G, int MT>
 static cudaError_t few_rows_mt(const Params &p, const CUtensorMap &tm, cudaStream_t s) {

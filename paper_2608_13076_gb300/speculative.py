@@ -19,6 +19,11 @@ until each sequence has produced `max_new` tokens or its end-of-sequence
 token, and reports verifier calls against tokens, the quantity the paper's
 cloud-call reduction is about (Sec. IV).
 
+ToyVerifierInt4 is the same model with its projections' weights and its KV cache in
+4 bits: spade_linear_w4 for the projections (the output projection adds the residual),
+spade_verify_qk_norm_rope_kv4 into a paged cache, spade_verify_attention_kv4 over it,
+the LM head without a commit and spade_kv_commit_kv4.
+
 This is a toy model for exercising and measuring the verify path end to end;
 it is not a trained model.
 """
@@ -29,8 +34,9 @@ from dataclasses import dataclass
 
 import torch
 
-from . import (accept_workspace, attn_workspace, qkv_workspace, spade_verify_accept_commit,
-               spade_verify_accept_sampling, spade_verify_attention, spade_verify_qkv_rope, status_tensor)
+from . import (accept_workspace, attn_workspace, int4, qkv_workspace, spade_kv_commit_kv4, spade_linear_w4,
+               spade_verify_accept, spade_verify_accept_commit, spade_verify_accept_sampling, spade_verify_attention,
+               spade_verify_attention_kv4, spade_verify_qk_norm_rope_kv4, spade_verify_qkv_rope, status_tensor)
 
 GREEDY = 0
 STOCHASTIC = 1
@@ -114,6 +120,60 @@ class ToyVerifier:
                                          kd, acc, tok, workspace=wsa, status=self.status, temperature=temperature,
                                          top_p=top_p, k_cache=self.k_cache, v_cache=self.v_cache,
                                          ctx_lens=self.ctx)
+        self.last_hidden = hidden
+        return acc, tok
+
+
+class ToyVerifierInt4(ToyVerifier):
+    """ToyVerifier's decoder with 4-bit projections (groups of `group` along the inputs), norms on
+    the query and key heads, and a paged 4-bit cache in pages of `page` slots."""
+
+    def __init__(self, cfg: ToyConfig, B: int, cap: int, seed: int, device, page: int = 64, group: int = 64):
+        super().__init__(cfg, B, cap, seed, device)
+        c, dev = cfg, self.device
+        del self.k_cache, self.v_cache
+        self.w_qkv, self.w_o = (int4.quantize(w, group) for w in (self.w_qkv, self.w_o))
+        self.q_norm = torch.ones(c.D, dtype=torch.bfloat16, device=dev)
+        self.k_norm = torch.ones_like(self.q_norm)
+        max_pages = -(-cap // page)
+        self.rope = int4.rope_table(c.rope_theta, c.D, max_pages * page, device=dev)
+        # Pages dealt to the sequences in turn, as a serving pool would end up.
+        self.pools = int4.kv4_pools(B * max_pages, c.Hkv, page, c.D, device=dev)
+        self.table = torch.arange(B * max_pages, dtype=torch.int32).reshape(max_pages, B).t().contiguous().to(dev)
+
+    def _heads(self, x, ctx, kd, cu_q, max_k):
+        """Query heads of rows x; their keys and values go into the cache at ctx + i."""
+        c, R = self.cfg, x.shape[0]
+        qkv = torch.empty((R, (c.Hq + 2 * c.Hkv) * c.D), dtype=torch.bfloat16, device=self.device)
+        spade_linear_w4(x, *self.w_qkv, qkv, status=self.status)
+        q = torch.empty((R, c.Hq, c.D), dtype=torch.bfloat16, device=self.device)
+        return spade_verify_qk_norm_rope_kv4(qkv, self.q_norm, self.k_norm, self.rope, q, *self.pools, self.table, ctx, kd,
+                                             cu_q, eps=1e-6, max_k=max_k, status=self.status)
+
+    def write_prefix(self, tokens, ctx, kd, cu_q, max_k):
+        self._heads(self.emb[tokens].contiguous(), ctx, kd, cu_q, max_k)
+
+    def verify(self, tokens, kd, cu_q, drafts, draft_probs, uniforms, mode, max_k, temperature=None, top_p=None):
+        c, R = self.cfg, tokens.numel()
+        x = self.emb[tokens].contiguous()
+        q = self._heads(x, self.ctx, kd, cu_q, max_k)
+        out = torch.empty_like(q)
+        slots = self.table.shape[1] * self.pools[0].shape[2]
+        ws = attn_workspace(self.B, c.Hq, c.Hkv, c.D, slots, max_k, device=self.device)
+        spade_verify_attention_kv4(q, *self.pools, self.table, self.ctx, kd, cu_q, out, None, max_k=max_k, workspace=ws,
+                                   status=self.status)
+        hidden = torch.empty_like(x)
+        spade_linear_w4(out.reshape(R, c.Hq * c.D), *self.w_o, hidden, x, status=self.status)
+        acc = torch.empty(self.B, dtype=torch.int32, device=self.device)
+        tok = torch.empty_like(acc)
+        wsa = accept_workspace(self.B, R, c.H, c.V, device=self.device)
+        if temperature is None and top_p is None:
+            spade_verify_accept(hidden, self.w_lm, drafts, draft_probs, uniforms, mode, cu_q, kd, acc, tok, workspace=wsa,
+                                status=self.status)
+        else:
+            spade_verify_accept_sampling(hidden, self.w_lm, drafts, draft_probs, uniforms, mode, cu_q, kd, acc, tok,
+                                         workspace=wsa, status=self.status, temperature=temperature, top_p=top_p)
+        spade_kv_commit_kv4(*self.pools, self.table, self.ctx, acc, kd, self.ctx, status=self.status)
         self.last_hidden = hidden
         return acc, tok
 

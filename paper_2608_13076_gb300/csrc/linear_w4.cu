@@ -214,8 +214,8 @@ __global__ void __launch_bounds__(kThreads) few_rows_kernel(const __grid_constan
 }
 
 // ---- more rows: tcgen05 with the weights in tensor memory ----------------------------------
-// y^T = W x^T again: 128 outputs on M, up to 128 rows of x on N, units of 128 k.  Two
-// threads unpack one output's unit (64 bytes of codes) to whole numbers in bf16 and store
+// y^T = W x^T again: 128 outputs on M, up to 128 rows of x on N, units of 128 k.  A
+// thread unpacks one output's unit (64 bytes of codes) to whole numbers in bf16 and stores
 // them to its lane of tensor memory, from where the MMA takes A (no shared-memory traffic
 // for W beyond its codes, and no loss of MMA rate at small N); x comes by TMA as B.  Each
 // group of k is accumulated apart, exact but for the fp32 sums, in one of two blocks of
@@ -241,7 +241,7 @@ struct Shape {
   static constexpr int kHalves = kWide ? 2 : 1;        // draining warps per lane quadrant
   static constexpr int kHalfRows = kRows / kHalves;    // sums of a draining thread
   static constexpr int kWarpDrain = 2, kWarpUnpack = 2 + 4 * kHalves;
-  static constexpr int kThreads = 32 * (kWarpUnpack + 8);
+  static constexpr int kThreads = 32 * (kWarpUnpack + 4);  // four unpacking warps
   static constexpr int kPerSm = kWide ? 1 : 2;
   static constexpr int kStages = 5;                    // copy ring (units)
   static constexpr int kBlock = !kWide && G <= 64 ? 2 : 1;  // groups accumulated side by side and drained together
@@ -290,10 +290,10 @@ __global__ void __launch_bounds__(Shape<G, kWide>::kThreads, Shape<G, kWide>::kP
     tma_prefetch_desc(&tm_x);
     for (int s = 0; s < S::kStages; ++s) {
       mbar_init(&s_full[s], 33);                   // the leader's copies, every lane's pairs
-      mbar_init(&s_empty[s], 9 + 4 * S::kHalves);  // eight unpacking warps, the draining ones and the MMAs
+      mbar_init(&s_empty[s], 4 + 4 * S::kHalves + 1);  // the unpacking and draining warps, and the MMAs
     }
     for (int s = 0; s < S::kA; ++s) {
-      mbar_init(&s_afull[s], 8);
+      mbar_init(&s_afull[s], 4);
       mbar_init(&s_afree[s], 1);
     }
     for (int s = 0; s < 2; ++s) {
@@ -413,11 +413,9 @@ __global__ void __launch_bounds__(Shape<G, kWide>::kThreads, Shape<G, kWide>::kP
       mbar_wait_unabortable(&s_drain, 0);
     }
   } else if (warp >= S::kWarpUnpack) {
-    // ---- unpacking: two threads per output, 64 k each ----
-    const int part = (warp - S::kWarpUnpack) / 4;
-    uint32_t it = 0;
-    for (int u = u0; u < u1; ++u, ++it) {
-      const int st = it % S::kStages, as = it % S::kA;
+    // ---- unpacking: a thread per output ----
+    for (int u = u0; u < u1; ++u) {
+      const int it = u - u0, st = it % S::kStages, as = it % S::kA;
       ok = mbar_wait_lean(&s_full[st], (it / S::kStages) & 1, &s_abort) &&
            mbar_wait_lean(&s_afree[as], ((it / S::kA) & 1) ^ 1, &s_abort);
       ok = __all_sync(0xffffffffu, ok);
@@ -427,11 +425,9 @@ __global__ void __launch_bounds__(Shape<G, kWide>::kThreads, Shape<G, kWide>::kP
       read_pairs<U>(smem + st * S::kStage + kCodes + S::kX, t, now);
       const uint8_t *row = smem + st * S::kStage + t * 64;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int j = 2 * part + h;  // 32 k
+      for (int j = 0; j < 4; ++j) {  // 32 k each
         const uint4 v = *reinterpret_cast<const uint4 *>(row + ((j ^ ((t >> 1) & 3)) << 4));
-        const uint32_t pair_bits = U == 1 ? now[0] : U == 2 ? (part ? now[U - 1] : now[0]) : (part ? now[(2 + h) % U] : now[h % U]);
-        const __nv_bfloat162 nz = __float2bfloat162_rn(-128.f - int4::pair_of(pair_bits).y);
+        const __nv_bfloat162 nz = __float2bfloat162_rn(-128.f - int4::pair_of(now[j * 32 / G]).y);
         uint32_t a[16];
         int4::unpack_bf16(v.x, nz, a);
         int4::unpack_bf16(v.y, nz, a + 4);

@@ -1,7 +1,7 @@
 // kv4_attention.cu -- attention of the k+1 verify positions over the paged 4-bit KV
 // cache (the verifier's single forward pass over the draft block: Sec. III-B
 // "Verification Stage", Algorithm 1 cloud step).
-// This file holds the C-ABI entry point: argument checks and the launch of
+// This file holds the C-ABI entry point: argument checks, tensor maps and the launch of
 // the kernel in kv4_attention_tc.cu.  Workspace, schedule and merge are those of the
 // attention over bf16 caches (attn_common.cuh).
 #include "internal.h"
@@ -67,10 +67,15 @@ extern "C" spade_status spade_verify_attention_kv4(
   const int64_t max_chunks = static_cast<int64_t>(units) * ((cap + attn::kChunk - 1) / attn::kChunk);
   p.num_ctas = static_cast<int>(max_chunks < sms ? max_chunks : sms);
 
-  const attn::Kv4Pool pool{static_cast<const uint8_t *>(k_codes), static_cast<const uint8_t *>(k_params),
-                           static_cast<const uint8_t *>(v_codes), static_cast<const uint8_t *>(v_params),
-                           num_pages * Hkv * page_size};
+  const uint64_t rows = static_cast<uint64_t>(num_pages) * Hkv * page_size;
+  CUtensorMap kc, vc, kp, vp;
+  if (!encode_tmap_bytes(&kc, k_codes, D / 2, rows, attn::kChunk, D / 2) ||
+      !encode_tmap_bytes(&vc, v_codes, D / 2, rows, attn::kChunk, D / 2) ||
+      !encode_tmap_words(&kp, k_params, attn::kChunk * (D / 64), rows / attn::kChunk) ||
+      !encode_tmap_words(&vp, v_params, attn::kChunk * (D / 64), rows / attn::kChunk))
+    return SPADE_ERR_CUDA;
   const int rows_max = G * (max_k + 1) < attn::kRowBlock ? G * (max_k + 1) : attn::kRowBlock;
-  const cudaError_t e = attn::launch_kv4(p, pool, (rows_max + 15) / 16 * 16, D, reinterpret_cast<cudaStream_t>(stream));
+  const cudaError_t e = attn::launch_kv4(p, kc, vc, kp, vp, (rows_max + 15) / 16 * 16, D,
+                                         reinterpret_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? SPADE_OK : cuda_fail(e, "verify_attention_kv4 launch");
 }

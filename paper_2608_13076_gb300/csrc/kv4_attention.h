@@ -5,14 +5,11 @@
 namespace spade {
 namespace attn {
 
-// The cache's pools, as bytes; `rows` slots of a head (num_pages * Hkv * page_size) in all.
-struct Kv4Pool {
-  const uint8_t *k_codes, *k_pairs, *v_codes, *v_pairs;
-  int rows;
-};
-
-// nr: rows of a unit, rounded up to 16.
-cudaError_t launch_kv4(const Params &p, const Kv4Pool &pool, int nr, int d, cudaStream_t stream);
+// Tensor maps: `kc`/`vc` fetch the codes of 64 slots of a head (encode_tmap_bytes),
+// `kp`/`vp` their (scale, zero) pairs (encode_tmap_words).  nr: rows of a unit, rounded
+// up to 16.
+cudaError_t launch_kv4(const Params &p, const CUtensorMap &kc, const CUtensorMap &vc, const CUtensorMap &kp,
+                       const CUtensorMap &vp, int nr, int d, cudaStream_t stream);
 
 }  // namespace attn
 }  // namespace spade

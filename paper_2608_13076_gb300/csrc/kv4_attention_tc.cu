@@ -18,7 +18,8 @@
 //    a whole number: one rounding, 2^-11) in shared memory, where the MMA reads them
 //    MN-major.  P is float16 too: P = 2^(s - m + 7) with the lazy maximum keeps it
 //    below 2^15, and what is 2^-32 of the largest weight or less is lost.
-//  * Warp roles: warp 0 copies codes and pairs (18 KB per 128 keys, four stages), warp 1
+//  * Warp roles: warp 0 copies codes and pairs (TMA; 18 KB per 128 keys, four
+//    stages, so that 18 KB stages cover the latency that 64 KB ones did), warp 1
 //    issues the MMAs, warps 2-9 run the softmax and the epilogue, warps 10-13 unpack
 //    keys, warps 14-17 values (96 registers a thread; the merge takes two rows at a
 //    time to stay within them).
@@ -31,7 +32,6 @@
 #include "attn_common.cuh"
 #include "int4.cuh"
 #include "kv4_attention.h"
-#include "launch.h"
 
 namespace spade {
 namespace attn {
@@ -123,7 +123,9 @@ SPADE_DEVICE uint4 load_codes(const uint8_t *codes, int t, int j) {
 
 template <int NR, int D>
 __global__ void __launch_bounds__(kThreads, 1)
-    verify_attention_kv4_kernel(const __grid_constant__ Params p, const __grid_constant__ Kv4Pool pool) {
+    verify_attention_kv4_kernel(const __grid_constant__ Params p, const __grid_constant__ CUtensorMap tm_kc,
+                                const __grid_constant__ CUtensorMap tm_vc, const __grid_constant__ CUtensorMap tm_kp,
+                                const __grid_constant__ CUtensorMap tm_vp) {
   static_assert(NR % 16 == 0 && NR >= 16 && NR <= kRowBlock, "MMA N must be 16..64, step 16");
   static_assert(D == 64 || D == 128, "head dim 64 or 128");
   constexpr int NG = D / 64;  // groups of a head
@@ -150,10 +152,13 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   if (tid == 0) { *s_abort = 0; *s_last = 0; }
   // Set-up that reads no input overlaps the previous kernel in the stream.
-  if (warp == 1) {
+  if (warp == 0 && lane < 2) {
+    tma_prefetch_desc(lane ? &tm_vc : &tm_kc);
+    tma_prefetch_desc(lane ? &tm_vp : &tm_kp);
+  } else if (warp == 1) {
     if (lane == 0) {
       for (int s = 0; s < kRing; ++s) {
-        mbar_init(&bars[kBarFull + s], 33);   // every lane's copies, and the chunk's description
+        mbar_init(&bars[kBarFull + s], 1);
         mbar_init(&bars[kBarEmpty + s], 8);   // the unpacking warps
       }
       for (int s = 0; s < kStages; ++s) {
@@ -223,77 +228,61 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t smem_base = smem_u32(smem);
 
   if (warp == 0) {
-    // ================== copies: a warp's asynchronous 16-byte pieces ==================
-    // (Tensor copies of a 64-slot slice, 4 KB of codes and 512 B of pairs, take an SM's copy
-    // engine about 340 cycles each, whatever is in flight: 3.4 TB/s.)
-    uint32_t st = 0, ph = 1;
+    // ============================ producer: TMA ============================
+    const bool leader = elect_one();
+    const uint64_t pol = l2_policy_evict_first();
+    sc.total = s_range->total;
+    sc.num_ctas = s_range->num_ctas;
+    const int64_t x_begin = s_range->x_begin, x_end = s_range->x_end;
+    constexpr uint32_t kSliceBytes = 2 * kChunk * (D / 2) + 2 * kChunk * NG * 4;
+    uint32_t st = 0, ph = 1, issued = 0;
     bool ok = true;
-    constexpr int kRowBytes = D / 2, kLanes = kRowBytes / 16;  // lanes of a slot's codes
-    // Where the lane's piece of eight (sixteen) slots goes: piece j of slot t at j ^ (t / 2) % 4
-    // (D = 64: j ^ (t / 4) % 2), so that reading a slot per lane meets no bank conflicts.
-    const uint32_t lane_to = (lane / kLanes) * kRowBytes +
-                             ((lane % kLanes) ^ (D == 128 ? (lane >> 3) & 3 : (lane >> 3) & 1)) * 16;
-    for (int64_t x = s_range->x_begin; ok && x < s_range->x_end;) {
-      sc.total = s_range->total;
-      sc.num_ctas = s_range->num_ctas;
-      const SegInfo si = x == s_range->x_begin ? *s_seg0 : next_seg_warp(sc, x, s_range->x_end, lane);
+    for (int64_t x = x_begin; ok && x < x_end;) {
+      const SegInfo si = x == x_begin ? *s_seg0 : next_seg_warp(sc, x, x_end, lane);
       const int n_here = uniform(si.n_here), nchunk = uniform(si.nchunk), ci = uniform(si.g.ci);
       if (n_here == 0) break;
       const int b = uniform(si.g.b), kvh = uniform(si.g.kvh);
       const int live = s_ctx[b] + s_kd[b] + 1;  // live slots of the sequence
-      // Each slice lies in one page; the lanes look up 32 slices at once.
-      auto rows_of = [&](int slice) {
-        return slice + lane < n_here ? paged_row(p, b, kvh, (ci + slice + lane) * kChunk) : 0;
-      };
-      int rows = rows_of(0), rows_next = 0;
       for (int c = 0; c < nchunk; ++c) {
         const int nsl = min(2, n_here - 2 * c);
         const int key0 = (ci + 2 * c) * kChunk;
-        if (c % 16 == 0) {
-          if (c) rows = rows_next;
-          rows_next = rows_of(2 * c + 32);
-        }
+        // Each slice lies in one page, found before the stage's wait.
+        const int row_a = uniform(paged_row(p, b, kvh, key0));
+        const int row_b = nsl == 2 ? uniform(paged_row(p, b, kvh, key0 + kChunk)) : 0;
+        uint8_t *stage = smem + Smem::RING + st * kStage;
         ok = warp_wait(&bars[kBarEmpty + st], ph, s_abort);
         if (!ok) break;
-        const uint32_t stage = smem_base + Smem::RING + st * kStage;
-        for (int i = 0; i < nsl; ++i) {
-          const int row = __shfl_sync(0xffffffffu, rows, (2 * c + i) % 32);
-          const bool real = row < pool.rows;  // (a page that is not in the pool reads as zeros)
-          const int64_t at = real ? row : 0;
-          const uint32_t size = real ? 16u : 0u;
-          const uint32_t codes = stage + i * kChunk * kRowBytes + lane_to;
-          const uint8_t *kc = pool.k_codes + at * kRowBytes + lane * 16, *vc = pool.v_codes + at * kRowBytes + lane * 16;
-#pragma unroll
-          for (int j = 0; j < kChunk * kRowBytes / 512; ++j) {
-            cp_async16(codes + j * 512, kc + j * 512, size);
-            cp_async16(codes + kCodes + j * 512, vc + j * 512, size);
-          }
-          if (lane < kChunk * NG * 4 / 16) {
-            const uint32_t pairs = stage + 2 * kCodes + i * kChunk * NG * 4 + lane * 16;
-            cp_async16(pairs, pool.k_pairs + at * (NG * 4) + lane * 16, size);
-            cp_async16(pairs + kPairs, pool.v_pairs + at * (NG * 4) + lane * 16, size);
-          }
-        }
-        cp_async_arrive(&bars[kBarFull + st]);
-        if (lane == 0) {
+        if (leader) {
           s_rmeta[st] = make_int2(min(nsl * kChunk, live - key0), (c == 0 ? kFirst : 0) | (c == nchunk - 1 ? kLast : 0));
-          mbar_arrive(&bars[kBarFull + st]);
+          mbar_arrive_expect_tx(&bars[kBarFull + st], nsl * kSliceBytes);
         }
+        for (int i = 0; i < nsl; ++i) {
+          const int row = i ? row_b : row_a;
+          uint8_t *codes = stage + i * kChunk * (D / 2);
+          uint8_t *pairs = stage + 2 * kCodes + i * kChunk * NG * 4;
+          if (leader) {
+            tma_load_2d(codes, &tm_kc, 0, row, &bars[kBarFull + st], pol);
+            tma_load_2d(pairs, &tm_kp, 0, row / kChunk, &bars[kBarFull + st], pol);
+            tma_load_2d(codes + kCodes, &tm_vc, 0, row, &bars[kBarFull + st], pol);
+            tma_load_2d(pairs + kPairs, &tm_vp, 0, row / kChunk, &bars[kBarFull + st], pol);
+          }
+        }
+        ++issued;
         if (++st == kRing) { st = 0; ph ^= 1u; }
       }
       x = si.seg_end;
     }
     if (ok) ok = warp_wait(&bars[kBarEmpty + st], ph, s_abort);
-    if (ok) {
-      cp_async_arrive(&bars[kBarFull + st]);
-      if (lane == 0) {
-        s_rmeta[st] = make_int2(0, kEnd);
-        mbar_arrive(&bars[kBarFull + st]);
-      }
-    } else if (lane == 0) {
-      atomicOr(p.status, SPADE_DEV_TIMEOUT);
+    if (ok && leader) {
+      s_rmeta[st] = make_int2(0, kEnd);
+      mbar_arrive(&bars[kBarFull + st]);
     }
-    cp_async_wait_all();  // every copy lands before the CTA's shared memory goes away
+    if (!ok && leader) {
+      atomicOr(p.status, SPADE_DEV_TIMEOUT);
+      // Drain: every copy issued must land before the CTA's smem goes away.
+      for (uint32_t j = (issued > kRing ? issued - kRing : 0); j < issued; ++j)
+        mbar_wait_unabortable(&bars[kBarFull + j % kRing], (j / kRing) & 1);
+    }
   } else if (warp == 1) {
     // ============================ MMA issuer ===============================
     constexpr uint32_t idesc_s = idesc_bf16_f32(128, NR);                          // A in tensor memory, K-major B
@@ -732,30 +721,42 @@ __global__ void __launch_bounds__(kThreads, 1)
 }
 
 template <int NR, int D>
-static cudaError_t launch_nr(const Params &p, const Kv4Pool &pool, cudaStream_t stream) {
+static cudaError_t launch_nr(const Params &p, const CUtensorMap &kc, const CUtensorMap &vc, const CUtensorMap &kp,
+                             const CUtensorMap &vp, cudaStream_t stream) {
   auto kern = verify_attention_kv4_kernel<NR, D>;
   static OncePerDevice once;
   const cudaError_t e = set_max_smem(once, Smem::BYTES, kern);
   if (e != cudaSuccess) return e;
-  return launch(kern, dim3(p.num_ctas), 1, kThreads, Smem::BYTES, stream, p, pool);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(p.num_ctas);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = Smem::BYTES;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kern, p, kc, vc, kp, vp);
 }
 
 }  // namespace kv4
 
-cudaError_t launch_kv4(const Params &p, const Kv4Pool &pool, int nr, int d, cudaStream_t stream) {
+cudaError_t launch_kv4(const Params &p, const CUtensorMap &kc, const CUtensorMap &vc, const CUtensorMap &kp,
+                       const CUtensorMap &vp, int nr, int d, cudaStream_t stream) {
   if (d == 64) {
     switch (nr) {
-      case 16: return kv4::launch_nr<16, 64>(p, pool, stream);
-      case 32: return kv4::launch_nr<32, 64>(p, pool, stream);
-      case 48: return kv4::launch_nr<48, 64>(p, pool, stream);
-      default: return kv4::launch_nr<64, 64>(p, pool, stream);
+      case 16: return kv4::launch_nr<16, 64>(p, kc, vc, kp, vp, stream);
+      case 32: return kv4::launch_nr<32, 64>(p, kc, vc, kp, vp, stream);
+      case 48: return kv4::launch_nr<48, 64>(p, kc, vc, kp, vp, stream);
+      default: return kv4::launch_nr<64, 64>(p, kc, vc, kp, vp, stream);
     }
   }
   switch (nr) {
-    case 16: return kv4::launch_nr<16, 128>(p, pool, stream);
-    case 32: return kv4::launch_nr<32, 128>(p, pool, stream);
-    case 48: return kv4::launch_nr<48, 128>(p, pool, stream);
-    default: return kv4::launch_nr<64, 128>(p, pool, stream);
+    case 16: return kv4::launch_nr<16, 128>(p, kc, vc, kp, vp, stream);
+    case 32: return kv4::launch_nr<32, 128>(p, kc, vc, kp, vp, stream);
+    case 48: return kv4::launch_nr<48, 128>(p, kc, vc, kp, vp, stream);
+    default: return kv4::launch_nr<64, 128>(p, kc, vc, kp, vp, stream);
   }
 }
 

@@ -391,17 +391,6 @@ __device__ __forceinline__ float warp_reduce_scatter(float (&v)[NP], int lane) {
   return r;
 }
 
-// 16-byte global -> shared copy (cp.async); src_bytes = 0 writes zeros.
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, uint32_t src_bytes) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(src_bytes)
-               : "memory");
-}
-__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void cp_async_wait() {
-  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
-}
-
 // One segment of a CTA's range: the part of one unit's cost span in
 // [x, seg_end); its real key slices are g.ci .. g.ci + n_here - 1.
 struct SegInfo {

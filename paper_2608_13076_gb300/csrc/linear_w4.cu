@@ -29,15 +29,20 @@ struct Params {
 // with masks), and the same part of the row of x.  Codes minus zero are whole numbers,
 // exact in bf16, and a group's products are summed apart and then scaled in fp32: nothing
 // of W is rounded.
-// The eight warps of a CTA take units of 128 k in turn, each with a ring of its own that
-// its first lane fills (TMA, 64 bytes of each output's row; the copy's swizzle makes the
-// fragments' reads free of bank conflicts for every group size), and add their sums in
-// shared memory in a fixed order.  Fragments straight from global memory kept the L1 busy
-// with 4-byte reads at group 32: 12288 x 4096 x 6 rows took 19.8 us.
-constexpr int kThreads = 256;
-constexpr int kWarps = kThreads / 32;
+// One CTA per SM takes a range of 16-output tiles; its warps share K, each with a span of
+// 256 k whose part of x stays in registers while the range's weights pass by (with eight
+// rows, fragments of x read again for every 32 outputs were as many bytes as the weights).
+// A warp has a ring of its own, filled by its lanes with 16-byte copies; the copies' places
+// make the fragments' reads free of bank conflicts for every group size.  Sums of a tile
+// wait in shared memory and are added over the warps in a fixed order.
+// 6 rows of 12288 x 4096, group 32: 9.9 us, 3.2 TB/s; 1 row of 57344 x 8192, group 128: 57 us,
+// 4.4 TB/s, where the copies alone take 43 us and the unpacking alone 43 us: both fill the SM.
+constexpr int kWarps = 16, kThreads = 32 * kWarps;
 constexpr int kUnit = 128;   // k per unit
-constexpr int kRing = 2;     // units in flight per warp
+constexpr int kSpan = 256;   // k of a warp: two units
+constexpr int kTile = 16;    // outputs of a tile
+constexpr int kRing = 2;     // spans in flight per warp (3 or 4: 1 to 5 % slower)
+constexpr int kHold = 8;     // tiles per warp whose sums wait in shared memory
 constexpr int kRows = 8;
 
 SPADE_DEVICE void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -66,150 +71,163 @@ SPADE_DEVICE void read_words(const uint8_t *rows, int r, int t, uint32_t (&w)[4]
   }
 }
 
-// The pairs of unit u's groups of one output (zeros past the last group).
-template <int U>
-SPADE_DEVICE void load_unit_pairs(const uint32_t *pairs, int u, int groups, bool whole, uint32_t (&p)[U]) {
-  const uint32_t *at = pairs + static_cast<int64_t>(u) * U;
-  if constexpr (U == 4) {
-    if (whole) {
-      const uint4 v = *reinterpret_cast<const uint4 *>(at);
-      p[0] = v.x; p[1] = v.y; p[2] = v.z; p[3] = v.w;
-      return;
-    }
-  } else if constexpr (U == 2) {
-    if (whole) {
-      const uint2 v = *reinterpret_cast<const uint2 *>(at);
-      p[0] = v.x; p[1] = v.y;
-      return;
-    }
-  }
-#pragma unroll
-  for (int q = 0; q < U; ++q) p[q] = u * U + q < groups ? at[q] : 0u;
-}
+// Shared memory of a CTA: the rings (codes, then pairs of a span), the sums that wait.
+template <int G>
+struct Few {
+  static constexpr int kPairs = kSpan / G;                     // pairs of an output in a span
+  static constexpr int kStage = kTile * (kSpan / 2 + kPairs * 4);
+  static constexpr int kRings = kWarps * kRing * kStage;
+  static constexpr int kSums = kWarps * 512;                   // one tile per warp
+};
 
-template <int G, int MT>
-__global__ void __launch_bounds__(kThreads) few_rows_kernel(const __grid_constant__ Params p,
-                                                            const __grid_constant__ CUtensorMap tm) {
+template <int G>
+__global__ void __launch_bounds__(kThreads, 1) few_rows_kernel(const __grid_constant__ Params p) {
+  using F = Few<G>;
   constexpr int W = G / 32, U = kUnit / G;  // words of a thread's part of a group; groups of a unit
-  constexpr int kStage = MT * 16 * 64;
-  extern __shared__ uint8_t smem_raw[];
-  uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-  __shared__ float s_sum[kWarps][MT * 16][kRows];
-  __shared__ uint64_t s_full[kWarps][kRing];
-  __shared__ int s_abort;
+  constexpr int kCodes = kTile * kSpan / 2;
+  extern __shared__ __align__(16) uint8_t smem[];
   const int warp = uniform_warp(), lane = threadIdx.x & 31;
   const int r = lane >> 2, t = lane & 3;
-  const int groups = p.K / G, units = (groups + U - 1) / U;
-  const int o0 = blockIdx.x * MT * 16;
-  uint8_t *ring = smem + warp * kRing * kStage;
-  uint64_t *full = s_full[warp];
-  if (threadIdx.x == 0) {
-    s_abort = 0;
-    tma_prefetch_desc(&tm);
-  }
-  if (lane == 0) {
-    for (int s = 0; s < kRing; ++s) mbar_init(&full[s], 1);
-    fence_mbar_init();
-  }
-  __syncthreads();
+  const int groups = p.K / G, spans = (p.K + kSpan - 1) / kSpan, row_bytes = p.K / 2;
+  uint8_t *ring = smem + warp * kRing * F::kStage;
+  float4 *sums = reinterpret_cast<float4 *>(smem + F::kRings);
+  // Warps along K (a power of two) and along the tiles.
+  const int kw = p.split, tw = kWarps / kw;
+  const int ki = warp & (kw - 1), ti = warp / kw;
+  const int tiles = (p.N - 1) / kTile + 1;
+  const int tile0 = static_cast<int>(static_cast<int64_t>(tiles) * blockIdx.x / gridDim.x);
+  const int tile1 = static_cast<int>(static_cast<int64_t>(tiles) * (blockIdx.x + 1) / gridDim.x);
+  const int slabs = ki < spans ? (spans - ki + kw - 1) / kw : 0;  // spans of this warp
+  // Tiles of this warp among the kHold * tw from `base` on.
+  auto tiles_from = [&](int base) { return min(kHold, (tile1 - base - ti + tw - 1) / tw); };
   griddep_wait();
   griddep_launch_dependents();
-  const int mine = warp < units ? (units - warp + kWarps - 1) / kWarps : 0;  // units of this warp
-  auto fill = [&](int i) {
-    uint64_t *bar = &full[i % kRing];
-    mbar_arrive_expect_tx(bar, kStage);
-    tma_load_2d(ring + (i % kRing) * kStage, &tm, (warp + i * kWarps) * (kUnit / 2), o0, bar, l2_policy_evict_first());
-  };
-  if (lane == 0)
-    for (int i = 0; i < min(kRing, mine); ++i) fill(i);
-  // Outputs past the end repeat the last one's pairs; what they give is not stored.
-  const uint32_t *pair[MT][2];
+
+  // ---- copies: steps in the order of the loops below, kRing ahead ----
+  // A lane copies pieces lane % 8 of rows lane / 8 + 0, 4, 8, 12: unit h = piece / 4 has a
+  // block of 64-byte rows, piece t of row r at place t ^ (r / 2 mod 4) of row r ^ h.
+  const bool whole = groups % F::kPairs == 0;
+  struct {
+    int base, slab, i;
+  } at = {slabs ? tile0 : tile1, 0, 0};
+  auto fetch = [&](int slot) {  // also counts a group where no step is left
+    if (at.base + ti < tile1) {
+      const int o0 = (at.base + ti + at.i * tw) * kTile, span = at.slab * kw + ki;
+      uint8_t *stage = ring + slot * F::kStage;
+      const int piece = lane & 7;
+      const bool in = span * (kSpan / 2) + piece * 16 < row_bytes;
+      const uint8_t *codes = reinterpret_cast<const uint8_t *>(p.codes) + (in ? span * (kSpan / 2) + piece * 16 : 0);
 #pragma unroll
-  for (int m = 0; m < MT; ++m)
+      for (int q = 0; q < 4; ++q) {
+        const int row = q * 4 + (lane >> 3), h = piece >> 2;
+        cp_async16(smem_u32(stage) + h * 1024 + (row ^ h) * 64 + (((piece & 3) ^ ((row >> 1) & 3)) << 4),
+                   codes + static_cast<int64_t>(min(o0 + row, p.N - 1)) * row_bytes, in ? 16 : 0);
+      }
+      // Pairs: two lanes per row, a unit's each.
+      const int row = lane >> 1, g0 = span * F::kPairs + (lane & 1) * U;
+      const uint32_t *from = p.pairs + static_cast<int64_t>(min(o0 + row, p.N - 1)) * groups;
+      const uint32_t to = smem_u32(stage) + kCodes + (row * F::kPairs + (lane & 1) * U) * 4;
+      if (whole) {
+        asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(from + g0), "n"(U * 4) : "memory");
+      } else {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) pair[m][h] = p.pairs + static_cast<int64_t>(min(o0 + m * 16 + h * 8 + r, p.N - 1)) * groups;
-  const bool whole = groups % U == 0;
-  const uint4 *x = reinterpret_cast<const uint4 *>(p.x + static_cast<int64_t>(min(r, p.R - 1)) * p.K) + W * t;
-  // Pairs and x of a unit, loaded while the one before it is worked on.
-  struct Rest {
-    uint32_t pr[MT][2][U];
-    uint4 xv[4];
-  };
-  Rest rest[2];
-  auto load_rest = [&](int u, Rest &a) {
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) load_unit_pairs<U>(pair[m][h], u, groups, whole, a.pr[m][h]);
-#pragma unroll
-    for (int q = 0; q < U; ++q)
-#pragma unroll
-      for (int e = 0; e < W; ++e)
-        a.xv[q * W + e] = u * U + q < groups ? x[(u * U + q) * (G / 8) + e] : make_uint4(0, 0, 0, 0);
-  };
-  if (mine) load_rest(warp, rest[0]);
-  float acc[MT][4] = {};
-  bool ok = true;
-  int issued = min(kRing, mine);
-  auto unit = [&](int i, const Rest &now, Rest &next) {
-    if (i + 1 < mine) load_rest(warp + (i + 1) * kWarps, next);
-    ok = __all_sync(0xffffffffu, mbar_wait_lean(&full[i % kRing], (i / kRing) & 1, &s_abort));
-    if (!ok) return;
-    uint32_t w[MT][2][4];
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) read_words<W>(ring + (i % kRing) * kStage + m * 1024, h * 8 + r, t, w[m][h]);
-    __syncwarp();
-    if (i + kRing < mine) {
-      if (lane == 0) fill(i + kRing);
-      ++issued;
-    }
-#pragma unroll
-    for (int q = 0; q < U; ++q) {
-#pragma unroll
-      for (int m = 0; m < MT; ++m) {
-        const float2 lo = int4::pair_of(now.pr[m][0][q]), hi = int4::pair_of(now.pr[m][1][q]);
-        const __nv_bfloat162 z0 = __float2bfloat162_rn(-128.f - lo.y), z1 = __float2bfloat162_rn(-128.f - hi.y);
-        float c[4] = {};
-#pragma unroll
-        for (int e = 0; e < W; ++e) {
-          uint32_t a[4], b[4];
-          int4::unpack_bf16(w[m][0][q * W + e], z0, a);
-          int4::unpack_bf16(w[m][1][q * W + e], z1, b);
-          const uint4 v = now.xv[q * W + e];
-          mma_bf16(c, a[0], b[0], a[1], b[1], v.x, v.y);
-          mma_bf16(c, a[2], b[2], a[3], b[3], v.z, v.w);
+        for (int q = 0; q < U; ++q) {
+          const bool have = g0 + q < groups;
+          asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to + q * 4), "l"(have ? from + g0 + q : from),
+                       "r"(have ? 4 : 0)
+                       : "memory");
         }
-        acc[m][0] = fmaf(lo.x, c[0], acc[m][0]);
-        acc[m][1] = fmaf(lo.x, c[1], acc[m][1]);
-        acc[m][2] = fmaf(hi.x, c[2], acc[m][2]);
-        acc[m][3] = fmaf(hi.x, c[3], acc[m][3]);
+      }
+      if (++at.i == tiles_from(at.base)) {
+        at.i = 0;
+        if (++at.slab == slabs) {
+          at.slab = 0;
+          at.base += kHold * tw;
+        }
       }
     }
+    cp_async_commit();
   };
-  for (int i = 0; ok && i < mine; i += 2) {
-    unit(i, rest[0], rest[1]);
-    if (ok && i + 1 < mine) unit(i + 1, rest[1], rest[0]);
-  }
-  if (!ok && lane == 0) {
-    atomicOr(p.status, SPADE_DEV_TIMEOUT);
-    // Every copy issued must land before the CTA's shared memory goes away.
-    for (int j = max(0, issued - kRing); j < issued; ++j) mbar_wait_unabortable(&full[j % kRing], (j / kRing) & 1);
-  }
 #pragma unroll
-  for (int m = 0; m < MT; ++m)
+  for (int s = 0; s < kRing; ++s) fetch(s);
+
+  const uint4 *x = reinterpret_cast<const uint4 *>(p.x + static_cast<int64_t>(min(r, p.R - 1)) * p.K) + W * t;
+  int slot = 0;
+  for (int base = tile0; base < tile1; base += kHold * tw) {
+    const int mine = tiles_from(base);
+    for (int slab = 0; slab < slabs; ++slab) {
+      const int g0 = (slab * kw + ki) * F::kPairs;
+      uint4 xv[8];
+      if (mine > 0) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) s_sum[warp][m * 16 + (e >> 1) * 8 + r][2 * t + (e & 1)] = acc[m][e];
-  __syncthreads();
-  for (int e = threadIdx.x; e < MT * 16 * kRows; e += kThreads) {
-    const int n = e / (MT * 16), o = e % (MT * 16);
-    if (n >= p.R || o0 + o >= p.N) continue;
-    float y = 0.f;
+        for (int q = 0; q < F::kPairs; ++q)
 #pragma unroll
-    for (int k = 0; k < kWarps; ++k) y += s_sum[k][o][n];
-    const int64_t at = static_cast<int64_t>(n) * p.N + o0 + o;
-    p.out[at] = __float2bfloat16_rn(y + (p.residual ? __bfloat162float(p.residual[at]) : 0.f));
+          for (int e = 0; e < W; ++e)
+            xv[q * W + e] = g0 + q < groups ? x[static_cast<int64_t>(g0 + q) * (G / 8) + e] : make_uint4(0, 0, 0, 0);
+      }
+      for (int i = 0; i < mine; ++i) {
+        cp_async_wait<kRing - 1>();
+        __syncwarp();
+        const uint8_t *stage = ring + slot * F::kStage;
+        uint32_t w[2][2][4], pairs[2][F::kPairs];
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) read_words<W>(stage + h * 1024, (m * 8 + r) ^ h, t, w[h][m]);
+          const uint32_t *pr = reinterpret_cast<const uint32_t *>(stage + kCodes) + (m * 8 + r) * F::kPairs;
+#pragma unroll
+          for (int q = 0; q < F::kPairs; q += 2) {
+            const uint2 v = *reinterpret_cast<const uint2 *>(pr + q);
+            pairs[m][q] = v.x;
+            pairs[m][q + 1] = v.y;
+          }
+        }
+        __syncwarp();
+        fetch(slot);
+        slot = slot + 1 == kRing ? 0 : slot + 1;
+        float acc[4] = {};
+#pragma unroll
+        for (int q = 0; q < F::kPairs; ++q) {
+          const float2 lo = int4::pair_of(pairs[0][q]), hi = int4::pair_of(pairs[1][q]);
+          const __nv_bfloat162 z0 = __float2bfloat162_rn(-128.f - lo.y), z1 = __float2bfloat162_rn(-128.f - hi.y);
+          float c[4] = {};
+#pragma unroll
+          for (int e = 0; e < W; ++e) {
+            uint32_t a[4], b[4];
+            int4::unpack_bf16(w[q / U][0][q % U * W + e], z0, a);
+            int4::unpack_bf16(w[q / U][1][q % U * W + e], z1, b);
+            const uint4 v = xv[q * W + e];
+            mma_bf16(c, a[0], b[0], a[1], b[1], v.x, v.y);
+            mma_bf16(c, a[2], b[2], a[3], b[3], v.z, v.w);
+          }
+          acc[0] = fmaf(lo.x, c[0], acc[0]);
+          acc[1] = fmaf(lo.x, c[1], acc[1]);
+          acc[2] = fmaf(hi.x, c[2], acc[2]);
+          acc[3] = fmaf(hi.x, c[3], acc[3]);
+        }
+        float4 &sum = sums[(i * kWarps + warp) * 32 + lane];
+        if (slab) {
+          const float4 s = sum;
+          acc[0] += s.x; acc[1] += s.y; acc[2] += s.z; acc[3] += s.w;
+        }
+        sum = make_float4(acc[0], acc[1], acc[2], acc[3]);
+      }
+    }
+    __syncthreads();
+    const int here = min(kHold * tw, tile1 - base);
+    for (int e = threadIdx.x; e < here * 128; e += kThreads) {
+      const int tile = e >> 7, l = (e >> 2) & 31, c = e & 3;
+      const int n = 2 * (l & 3) + (c & 1);
+      const int64_t o = static_cast<int64_t>(base + tile) * kTile + (c >> 1) * 8 + (l >> 2);
+      if (n >= p.R || o >= p.N) continue;
+      // Tile `tile` is number tile / tw of the warps (tile mod tw) * kw + 0 .. kw - 1.
+      const float *from = reinterpret_cast<const float *>(sums) + ((tile / tw) * kWarps + (tile % tw) * kw) * 128 + (e & 127);
+      float y = 0.f;
+      for (int k = 0; k < min(kw, spans); ++k) y += from[k * 128];
+      const int64_t to = n * static_cast<int64_t>(p.N) + o;
+      p.out[to] = __float2bfloat16_rn(y + (p.residual ? __bfloat162float(p.residual[to]) : 0.f));
+    }
+    if (base + kHold * tw < tile1) __syncthreads();
   }
 }
 
@@ -338,8 +356,7 @@ __global__ void __launch_bounds__(Shape<G, kWide>::kThreads, Shape<G, kWide>::kP
       if (!ok) break;
       uint8_t *stage = smem + st * S::kStage;
       // Pairs: four outputs per lane, by asynchronous copies that arrive on the stage's barrier
-      // themselves.  (Loads into registers ahead of time do not work here: a warp's arrivals
-      // release, and so wait for every load that it has in flight.  They cost 1300 cycles a unit.)
+      // themselves.
 #pragma unroll
       for (int r = lane; r < kOut; r += 32) {
         const uint32_t *from = p.pairs + static_cast<int64_t>(min(o0 + r, p.N - 1)) * groups + u * U;
@@ -552,20 +569,19 @@ __global__ void __launch_bounds__(Shape<G, kWide>::kThreads, Shape<G, kWide>::kP
 
 }  // namespace tc
 
-template <int G, int MT>
-static cudaError_t few_rows_mt(const Params &p, const CUtensorMap &tm, cudaStream_t s) {
-  constexpr int kBytes = kWarps * kRing * MT * 1024 + 1024;
-  static OncePerDevice once;
-  const cudaError_t e = set_max_smem(once, kBytes, few_rows_kernel<G, MT>);
-  if (e != cudaSuccess) return e;
-  return launch(few_rows_kernel<G, MT>, dim3((static_cast<unsigned>(p.N) + MT * 16 - 1) / (MT * 16)), 1, kThreads, kBytes, s,
-                p, tm);
-}
-// 32 outputs a CTA halve the reads of x; 16 fill the SMs sooner.
-static bool wide_tiles(int N, int sms) { return (static_cast<unsigned>(N) + 31) / 32 >= 2u * sms; }
 template <int G>
-static cudaError_t few_rows(const Params &p, const CUtensorMap &tm, bool wide, cudaStream_t s) {
-  return wide ? few_rows_mt<G, 2>(p, tm, s) : few_rows_mt<G, 1>(p, tm, s);
+static cudaError_t few_rows(Params p, int sms, cudaStream_t s) {
+  using F = Few<G>;
+  static OncePerDevice once;
+  const cudaError_t e = set_max_smem(once, F::kRings + kHold * F::kSums, few_rows_kernel<G>);
+  if (e != cudaSuccess) return e;
+  const int tiles = (p.N - 1) / kTile + 1, spans = (p.K + kSpan - 1) / kSpan;
+  const int grid = tiles < sms ? tiles : sms, most = (tiles - 1) / grid + 1;  // tiles of a CTA
+  // Warps along K: as many as have a span; with a single tile all of them share it anyway.
+  p.split = kWarps;
+  while (p.split / 2 >= spans) p.split /= 2;
+  const int each = (most - 1) / (kWarps / p.split) + 1;  // tiles of a warp
+  return launch(few_rows_kernel<G>, dim3(grid), 1, kThreads, F::kRings + (each < kHold ? each : kHold) * F::kSums, s, p);
 }
 
 template <int G, bool kWide>
@@ -625,11 +641,9 @@ extern "C" spade_status spade_linear_w4(const void *x, const void *codes, const 
   CUtensorMap w;
   cudaError_t e;
   if (R <= w4::kRows) {
-    const bool wide = w4::wide_tiles(N, sms);
-    if (!encode_tmap_bytes(&w, codes, K / 2, N, wide ? 32 : 16, 64)) return SPADE_ERR_CUDA;
-    e = group == 128 ? w4::few_rows<128>(p, w, wide, s)
-        : group == 64 ? w4::few_rows<64>(p, w, wide, s)
-                      : w4::few_rows<32>(p, w, wide, s);
+    e = group == 128 ? w4::few_rows<128>(p, sms, s)
+        : group == 64 ? w4::few_rows<64>(p, sms, s)
+                      : w4::few_rows<32>(p, sms, s);
   } else {
     const bool wide = R > w4::tc::kNarrow;
     const int most = wide ? w4::tc::kMost : w4::tc::kNarrow;

@@ -239,10 +239,14 @@ __global__ void __launch_bounds__(kThreads, 1) few_rows_kernel(const __grid_cons
 // group of k is accumulated apart, exact but for the fp32 sums, in one of two blocks of
 // columns, and the draining warps take the other under the outputs' scales into registers.
 // Bound by the weights' bytes at few rows, then by the instructions that unpack (each row
-// tile unpacks W again) and drain, with the MMAs close behind at 128 rows.  Up to 32 rows
-// a tile two CTAs share an SM, so that one's waits are the other's work; wider tiles take
-// an SM each, since halving the unpacking is worth more (389 rows of 7168 x 5120 in tiles
-// of 56 rows, two CTAs: 99 us).
+// tile unpacks W again) and drain (each group of k once), with the MMAs close behind: a unit
+// of 128 x 128 sums takes 950 cycles at group 128, its MMAs 512.  Up to 32 rows a tile two
+// CTAs share an SM, so that one's waits are the other's work; wider tiles take an SM each,
+// since halving the unpacking is worth more (389 rows of 7168 x 5120 in tiles of 56 rows, two
+// CTAs: 99 us).  At group 128 a CTA can take two tiles of outputs: they share the copies of x
+// and a CTA's start and end, with three blocks of sums and two of unpacked weights in turn.
+// 20 rows of 8192 x 8192, group 64: 16.1 us; 389 rows of 7168 x 5120, group 128: 43.9 us, and
+// 1024 rows of 12288 x 4096: 112 us (650 and 920 TFLOP/s).
 // Where the tiles do not fill the GPU, a cluster of 2, 4 or 8 CTAs takes a tile's units
 // in equal parts and adds the sums through distributed shared memory in a fixed order.
 namespace tc {
@@ -253,25 +257,29 @@ constexpr int kMaxSplit = 8;
 constexpr int kNarrow = 32, kMost = 128;        // rows of a narrow and of a wide tile, at most
 constexpr int kMaxStages = 6, kMaxA = 4;
 
-template <int G, bool kWide>
+template <int G, bool kWide, int kTiles>
 struct Shape {
   static constexpr int kRows = kWide ? kMost : kNarrow;  // most rows of a tile
-  static constexpr int kHalves = kWide ? 2 : 1;        // draining warps per lane quadrant
+  static constexpr int kM = kTiles;                    // tiles of outputs that share a tile of x
+  static constexpr int kHalves = kWide ? 2 : 1;        // draining warps per lane quadrant and tile of outputs
   static constexpr int kHalfRows = kRows / kHalves;    // sums of a draining thread
-  static constexpr int kWarpDrain = 2, kWarpUnpack = 2 + 4 * kHalves;
+  static constexpr int kWarpDrain = 2, kWarpUnpack = 2 + 4 * kHalves * kM;
   static constexpr int kThreads = 32 * (kWarpUnpack + 4);  // four unpacking warps
   static constexpr int kPerSm = kWide ? 1 : 2;
-  static constexpr int kStages = 5;                    // copy ring (units)
+  static constexpr int kStages = kM == 2 ? 4 : 5;        // copy ring (units)
+  static constexpr int kChunk = kM == 2 ? 16 : 32;       // sums that a draining thread reads at a time
   static constexpr int kBlock = !kWide && G <= 64 ? 2 : 1;  // groups accumulated side by side and drained together
-  static constexpr int kA = kWide ? 4 : kBlock == 2 ? 2 : 3;  // unpacked units
+  static constexpr int kD = kM == 2 ? 3 : 2;           // blocks of columns that sums go to
+  static constexpr int kA = kM == 2 ? 2 : kWide ? 4 : kBlock == 2 ? 2 : 3;  // unpacked units
   static constexpr uint32_t kTmemCols = kWide ? 512 : 256;
-  static constexpr uint32_t kColD = 0, kColA = 2 * kBlock * kRows;
+  static constexpr uint32_t kColD = 0, kColA = kD * kBlock * kRows;
   static constexpr int kX = kRows * 256;               // a unit of x: two slabs of [rows][64 k]
-  static constexpr int kPairs = kOut * (kUnit / G) * 4;  // a unit's (scale, zero) pairs
-  static constexpr int kStage = (kCodes + kX + kPairs + 1023) / 1024 * 1024;
+  static constexpr int kPairs = kM * kOut * (kUnit / G) * 4;  // a unit's (scale, zero) pairs
+  static constexpr int kAtX = kM * kCodes, kAtPairs = kAtX + kX;
+  static constexpr int kStage = (kAtPairs + kPairs + 1023) / 1024 * 1024;
   static constexpr int kBytes = kStages * kStage + 1024;
   static_assert(kColA + kA * 64 <= kTmemCols, "tensor memory");
-  static_assert(kOut * kRows * 4 <= kStages * kStage, "a split's sums reuse the ring");
+  static_assert(kM * kOut * kRows * 4 <= kStages * kStage, "a split's sums reuse the ring");
   static_assert(kStages <= kMaxStages && kA <= kMaxA, "barriers");
 };
 
@@ -289,15 +297,15 @@ SPADE_DEVICE void read_pairs(const uint8_t *pairs, int t, uint32_t (&p)[U]) {
   }
 }
 
-template <int G, bool kWide>
-__global__ void __launch_bounds__(Shape<G, kWide>::kThreads, Shape<G, kWide>::kPerSm)
+template <int G, bool kWide, int kTiles>
+__global__ void __launch_bounds__(Shape<G, kWide, kTiles>::kThreads, Shape<G, kWide, kTiles>::kPerSm)
     rows_kernel(const __grid_constant__ Params p, const __grid_constant__ CUtensorMap tm_w,
                 const __grid_constant__ CUtensorMap tm_x) {
-  using S = Shape<G, kWide>;
+  using S = Shape<G, kWide, kTiles>;
   constexpr int U = kUnit / G;
   extern __shared__ uint8_t smem_raw[];
   uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-  __shared__ uint64_t s_full[kMaxStages], s_empty[kMaxStages], s_afull[kMaxA], s_afree[kMaxA], s_dfull[2], s_dfree[2],
+  __shared__ uint64_t s_full[kMaxStages], s_empty[kMaxStages], s_afull[kMaxA], s_afree[kMaxA], s_dfull[3], s_dfree[3],
       s_drain;
   __shared__ int s_abort;
   __shared__ uint32_t s_tmem;
@@ -308,13 +316,13 @@ __global__ void __launch_bounds__(Shape<G, kWide>::kThreads, Shape<G, kWide>::kP
     tma_prefetch_desc(&tm_x);
     for (int s = 0; s < S::kStages; ++s) {
       mbar_init(&s_full[s], 33);                   // the leader's copies, every lane's pairs
-      mbar_init(&s_empty[s], 4 + 4 * S::kHalves + 1);  // the unpacking and draining warps, and the MMAs
+      mbar_init(&s_empty[s], 4 + 4 * S::kHalves * S::kM + 1);  // the unpacking and draining warps, and the MMAs
     }
     for (int s = 0; s < S::kA; ++s) {
       mbar_init(&s_afull[s], 4);
       mbar_init(&s_afree[s], 1);
     }
-    for (int s = 0; s < 2; ++s) {
+    for (int s = 0; s < S::kD; ++s) {
       mbar_init(&s_dfull[s], 1);
       mbar_init(&s_dfree[s], 4 * S::kHalves);
     }
@@ -331,14 +339,15 @@ __global__ void __launch_bounds__(Shape<G, kWide>::kThreads, Shape<G, kWide>::kP
   const uint32_t tmem = s_tmem;
   const int groups = p.K / G, units = (groups + U - 1) / U;
   const int split = p.split, rank = split > 1 ? static_cast<int>(cluster_ctarank()) : 0;
-  const int o0 = static_cast<int>(blockIdx.x / split) * kOut, n0 = blockIdx.y * p.tile_rows;
+  const int o0 = static_cast<int>(blockIdx.x / split) * (S::kM * kOut), n0 = blockIdx.y * p.tile_rows;
   const int n = p.tile_n;  // rows of x in the MMA: the tile's, rounded up to 16
   const int u0 = static_cast<int>(static_cast<int64_t>(units) * rank / split);
   const int u1 = static_cast<int>(static_cast<int64_t>(units) * (rank + 1) / split);
   const int t = (warp & 3) * 32 + lane;                       // output of the unpacking and draining threads
   const uint32_t tlane = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
   const int half_rows = kWide ? (n / 16 + 1) / 2 * 16 : n;    // rows of the first draining half
-  const int r_lo = kWide && warp >= S::kWarpDrain + 4 ? half_rows : 0;  // this thread's first row (draining)
+  const int dm = (warp - S::kWarpDrain) / (4 * S::kHalves);   // (draining) the warp's tile of outputs
+  const int r_lo = kWide && ((warp - S::kWarpDrain) & 4) ? half_rows : 0;  // and its thread's first row
   const int my_rows = min(half_rows, n - r_lo);
   griddep_wait();
   griddep_launch_dependents();
@@ -358,9 +367,9 @@ __global__ void __launch_bounds__(Shape<G, kWide>::kThreads, Shape<G, kWide>::kP
       // Pairs: four outputs per lane, by asynchronous copies that arrive on the stage's barrier
       // themselves.
 #pragma unroll
-      for (int r = lane; r < kOut; r += 32) {
+      for (int r = lane; r < S::kM * kOut; r += 32) {
         const uint32_t *from = p.pairs + static_cast<int64_t>(min(o0 + r, p.N - 1)) * groups + u * U;
-        const uint32_t to = smem_u32(stage + kCodes + S::kX) + r * (U * 4);
+        const uint32_t to = smem_u32(stage + S::kAtPairs) + r * (U * 4);
         if (groups % U == 0) {
           asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(from), "n"(U * 4) : "memory");
         } else {
@@ -374,10 +383,12 @@ __global__ void __launch_bounds__(Shape<G, kWide>::kThreads, Shape<G, kWide>::kP
       }
       asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&s_full[st])) : "memory");
       if (leader) {
-        mbar_arrive_expect_tx(&s_full[st], kCodes + n * 256);
-        tma_load_2d(stage, &tm_w, u * (kUnit / 2), o0, &s_full[st], pol_w);
-        tma_load_2d(stage + kCodes, &tm_x, u * kUnit, n0, &s_full[st], pol);
-        tma_load_2d(stage + kCodes + S::kX / 2, &tm_x, u * kUnit + 64, n0, &s_full[st], pol);
+        mbar_arrive_expect_tx(&s_full[st], S::kM * kCodes + n * 256);
+#pragma unroll
+        for (int m = 0; m < S::kM; ++m)
+          tma_load_2d(stage + m * kCodes, &tm_w, u * (kUnit / 2), o0 + m * kOut, &s_full[st], pol_w);
+        tma_load_2d(stage + S::kAtX, &tm_x, u * kUnit, n0, &s_full[st], pol);
+        tma_load_2d(stage + S::kAtX + S::kX / 2, &tm_x, u * kUnit + 64, n0, &s_full[st], pol);
       }
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
@@ -394,33 +405,44 @@ __global__ void __launch_bounds__(Shape<G, kWide>::kThreads, Shape<G, kWide>::kP
       ok = __all_sync(0xffffffffu, mbar_wait_lean(bar, parity, &s_abort)) && ok;
     };
     for (int u = u0; ok && u < u1; ++u, ++it) {
-      const int st = it % S::kStages, as = it % S::kA;
+      const int st = it % S::kStages;
       wait(&s_full[st], (it / S::kStages) & 1);
-      wait(&s_afull[as], (it / S::kA) & 1);
-      if (!ok) break;
-      const uint64_t dx = smem_desc_sw128(base + st * S::kStage + kCodes);
+      if constexpr (S::kM == 1) {
+        wait(&s_afull[it % S::kA], (it / S::kA) & 1);
+        if (!ok) break;
+      }
+      const uint64_t dx = smem_desc_sw128(base + st * S::kStage + S::kAtX);
       const int ng = min(U, groups - u * U);
 #pragma unroll
       for (int q0 = 0; q0 < U; q0 += S::kBlock) {
         if (q0 >= ng) break;
-        const int db = bi & 1;
-        wait(&s_dfree[db], ((bi / 2) & 1) ^ 1);
-        tc_fence_after();
 #pragma unroll
-        for (int q = q0; q < q0 + S::kBlock; ++q) {  // (a group past the last: zeros)
-          const uint32_t d = tmem + S::kColD + (db * S::kBlock + q - q0) * S::kRows;
+        for (int m = 0; m < S::kM; ++m) {
+          const uint32_t ai = it * S::kM + m;
+          const int as = ai % S::kA;
+          if (S::kM > 1 && q0 == 0) wait(&s_afull[as], (ai / S::kA) & 1);
+          const int db = bi % S::kD;
+          wait(&s_dfree[db], ((bi / S::kD) & 1) ^ 1);
+          tc_fence_after();
 #pragma unroll
-          for (int k = 0; k < G / 16; ++k) {
-            const int kk = q * (G / 16) + k;  // four per 64-k slab
-            const uint32_t off = ((kk / 4) * (S::kX / 2) + (kk % 4) * 32) >> 4;
-            if (leader) tc_mma_f16_ta(d, tmem + S::kColA + as * 64 + kk * 8, dx + off, idesc, k > 0);
+          for (int q = q0; q < q0 + S::kBlock; ++q) {  // (a group past the last: zeros)
+            const uint32_t d = tmem + S::kColD + (db * S::kBlock + q - q0) * S::kRows;
+#pragma unroll
+            for (int k = 0; k < G / 16; ++k) {
+              const int kk = q * (G / 16) + k;  // four per 64-k slab
+              const uint32_t off = ((kk / 4) * (S::kX / 2) + (kk % 4) * 32) >> 4;
+              if (leader) tc_mma_f16_ta(d, tmem + S::kColA + as * 64 + kk * 8, dx + off, idesc, k > 0);
+            }
           }
+          if (leader) {
+            tc_commit(&s_dfull[db]);
+            if (S::kM > 1 && q0 + S::kBlock >= ng) tc_commit(&s_afree[as]);
+          }
+          ++bi;
         }
-        if (leader) tc_commit(&s_dfull[db]);
-        ++bi;
       }
-      if (leader) {
-        tc_commit(&s_afree[as]);
+      if (leader && ok) {
+        if constexpr (S::kM == 1) tc_commit(&s_afree[it % S::kA]);
         tc_commit(&s_empty[st]);
       }
     }
@@ -432,33 +454,35 @@ __global__ void __launch_bounds__(Shape<G, kWide>::kThreads, Shape<G, kWide>::kP
   } else if (warp >= S::kWarpUnpack) {
     // ---- unpacking: a thread per output ----
     for (int u = u0; u < u1; ++u) {
-      const int it = u - u0, st = it % S::kStages, as = it % S::kA;
-      ok = mbar_wait_lean(&s_full[st], (it / S::kStages) & 1, &s_abort) &&
-           mbar_wait_lean(&s_afree[as], ((it / S::kA) & 1) ^ 1, &s_abort);
-      ok = __all_sync(0xffffffffu, ok);
-      if (!ok) break;
-      tc_fence_after();
-      uint32_t now[U];
-      read_pairs<U>(smem + st * S::kStage + kCodes + S::kX, t, now);
-      const uint8_t *row = smem + st * S::kStage + t * 64;
+      const int it = u - u0, st = it % S::kStages;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {  // 32 k each
-        const uint4 v = *reinterpret_cast<const uint4 *>(row + ((j ^ ((t >> 1) & 3)) << 4));
-        const __nv_bfloat162 nz = __float2bfloat162_rn(-128.f - int4::pair_of(now[j * 32 / G]).y);
-        uint32_t a[16];
-        int4::unpack_bf16(v.x, nz, a);
-        int4::unpack_bf16(v.y, nz, a + 4);
-        int4::unpack_bf16(v.z, nz, a + 8);
-        int4::unpack_bf16(v.w, nz, a + 12);
-        tmem_st16(tlane + S::kColA + as * 64 + j * 16, a);
+      for (int m = 0; m < S::kM; ++m) {
+        const int ai = it * S::kM + m, as = ai % S::kA;
+        ok = (m || mbar_wait_lean(&s_full[st], (it / S::kStages) & 1, &s_abort)) && mbar_wait_lean(&s_afree[as], ((ai / S::kA) & 1) ^ 1, &s_abort);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        tc_fence_after();
+        uint32_t now[U];
+        read_pairs<U>(smem + st * S::kStage + S::kAtPairs, m * kOut + t, now);
+        const uint8_t *row = smem + st * S::kStage + m * kCodes + t * 64;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {  // 32 k each
+          const uint4 v = *reinterpret_cast<const uint4 *>(row + ((j ^ ((t >> 1) & 3)) << 4));
+          const __nv_bfloat162 nz = __float2bfloat162_rn(-128.f - int4::pair_of(now[j * 32 / G]).y);
+          uint32_t a[16];
+          int4::unpack_bf16(v.x, nz, a);
+          int4::unpack_bf16(v.y, nz, a + 4);
+          int4::unpack_bf16(v.z, nz, a + 8);
+          int4::unpack_bf16(v.w, nz, a + 12);
+          tmem_st16(tlane + S::kColA + as * 64 + j * 16, a);
+        }
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&s_afull[as]);
       }
-      tmem_wait_st();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) {
-        mbar_arrive(&s_afull[as]);
-        mbar_arrive(&s_empty[st]);
-      }
+      if (!ok) break;
+      if (lane == 0) mbar_arrive(&s_empty[st]);
     }
   } else {
     // ---- draining: a group's sums under the outputs' scales ----
@@ -471,13 +495,14 @@ __global__ void __launch_bounds__(Shape<G, kWide>::kThreads, Shape<G, kWide>::kP
 #pragma unroll
       for (int q0 = 0; q0 < U; q0 += S::kBlock) {
         if (q0 >= ng) break;
-        const int db = bi & 1;
+        const uint32_t bm = S::kM == 1 ? bi : bi * S::kM + dm;
+        const int db = bm % S::kD;
         // (The sums come after their unit's copies; the first wait is for the reads of those.)
         if (q0 == 0) ok = mbar_wait_lean(&s_full[st], (it / S::kStages) & 1, &s_abort);
-        ok = __all_sync(0xffffffffu, ok && mbar_wait_lean(&s_dfull[db], (bi / 2) & 1, &s_abort));
+        ok = __all_sync(0xffffffffu, ok && mbar_wait_lean(&s_dfull[db], (bm / S::kD) & 1, &s_abort));
         if (!ok) break;
         tc_fence_after();
-        if (q0 == 0) read_pairs<U>(smem + st * S::kStage + kCodes + S::kX, t, now);
+        if (q0 == 0) read_pairs<U>(smem + st * S::kStage + S::kAtPairs, (S::kM == 1 ? 0 : dm * kOut) + t, now);
 #pragma unroll
         for (int q = q0; q < q0 + S::kBlock; ++q) {
           if (q >= ng) break;
@@ -485,14 +510,14 @@ __global__ void __launch_bounds__(Shape<G, kWide>::kThreads, Shape<G, kWide>::kP
           const F2 ss = f2(s, s);
           const uint32_t from = tlane + S::kColD + (db * S::kBlock + q - q0) * S::kRows + r_lo;
 #pragma unroll
-          for (int k = 0; k < S::kHalfRows; k += 32) {
+          for (int k = 0; k < S::kHalfRows; k += S::kChunk) {
             if (k >= my_rows) break;
-            uint32_t y[32];
+            uint32_t y[S::kChunk];
 #pragma unroll
-            for (int j = 0; j < 32; j += 8) tmem_ld8(from + k + j, y + j);  // (columns past the tile's rows: unused)
+            for (int j = 0; j < S::kChunk; j += 8) tmem_ld8(from + k + j, y + j);  // (columns past the tile's rows: unused)
             tmem_wait_ld();
 #pragma unroll
-            for (int e = 0; e < 32; e += 2)
+            for (int e = 0; e < S::kChunk; e += 2)
               sum[(k + e) / 2] = f2_fma(f2(__uint_as_float(y[e]), __uint_as_float(y[e + 1])), ss, sum[(k + e) / 2]);
           }
         }
@@ -510,14 +535,15 @@ __global__ void __launch_bounds__(Shape<G, kWide>::kThreads, Shape<G, kWide>::kP
 
   const int rows = min(p.tile_rows, p.R - n0);
   const bool drains = warp >= S::kWarpDrain && warp < S::kWarpUnpack;
-  if (split == 1) {
-    if (drains && o0 + t < p.N) {
+  if (S::kM == 2 || split == 1) {
+    const int o = o0 + dm * kOut + t;
+    if (drains && o < p.N) {
 #pragma unroll
       for (int r = 0; r < S::kHalfRows; ++r) {
         if (r >= my_rows || r_lo + r >= rows) break;
         float y[2];
         f2_split(sum[r / 2], y[0], y[1]);
-        const int64_t at = static_cast<int64_t>(n0 + r_lo + r) * p.N + o0 + t;
+        const int64_t at = static_cast<int64_t>(n0 + r_lo + r) * p.N + o;
         p.out[at] = __float2bfloat16_rn(y[r & 1] + (p.residual ? __bfloat162float(p.residual[at]) : 0.f));
       }
     }
@@ -584,24 +610,26 @@ static cudaError_t few_rows(Params p, int sms, cudaStream_t s) {
   return launch(few_rows_kernel<G>, dim3(grid), 1, kThreads, F::kRings + (each < kHold ? each : kHold) * F::kSums, s, p);
 }
 
-template <int G, bool kWide>
+template <int G, bool kWide, int kTiles>
 static cudaError_t rows(const Params &p, const CUtensorMap &w, const CUtensorMap &x, cudaStream_t s) {
-  using S = tc::Shape<G, kWide>;
+  using S = tc::Shape<G, kWide, kTiles>;
   static OncePerDevice once;
-  const cudaError_t e = set_max_smem(once, S::kBytes, tc::rows_kernel<G, kWide>);
+  const cudaError_t e = set_max_smem(once, S::kBytes, tc::rows_kernel<G, kWide, kTiles>);
   if (e != cudaSuccess) return e;
-  const unsigned tiles = (static_cast<unsigned>(p.N) + tc::kOut - 1) / tc::kOut;
+  const unsigned tiles = (static_cast<unsigned>(p.N) - 1) / (S::kM * tc::kOut) + 1;
   const dim3 grid(tiles * p.split, (p.R + p.tile_rows - 1) / p.tile_rows);
-  return launch(tc::rows_kernel<G, kWide>, grid, p.split, S::kThreads, S::kBytes, s, p, w, x);
+  return launch(tc::rows_kernel<G, kWide, kTiles>, grid, p.split, S::kThreads, S::kBytes, s, p, w, x);
 }
 
-// CTAs that share a tile's units: those that fill the GPU's slots in the fewest rounds
-// per part, of at least four units each; the fewer the better.
+// CTAs that share a tile's units, of at least four each: those that finish first, when a
+// CTA takes as long as its units and 8 more (its start, its first copies, its sums), and
+// the GPU has `slots` of them at a time; the fewer the better.
 static int split_of(int64_t tiles, int units, int slots) {
+  constexpr int kFixed = 8;
   int best = 1;
-  double cost = 1e30;
+  int64_t cost = INT64_MAX;
   for (int s = 1; s <= tc::kMaxSplit && (s == 1 || units >= 4 * s); s *= 2) {
-    const double c = static_cast<double>((tiles * s + slots - 1) / slots) / s;
+    const int64_t c = ((tiles * s - 1) / slots + 1) * ((units - 1) / s + 1 + kFixed);
     if (c < cost) {
       cost = c;
       best = s;
@@ -651,20 +679,29 @@ extern "C" spade_status spade_linear_w4(const void *x, const void *codes, const 
     if (row_tiles > 65535) return fail(SPADE_ERR_SHAPE, "spade_linear_w4: R = %d exceeds %d rows per call", R, 65535 * most);
     p.tile_rows = (R - 1) / row_tiles + 1;
     p.tile_n = (p.tile_rows + 15) / 16 * 16;
-    const int64_t tiles = (static_cast<int64_t>(N) + w4::tc::kOut - 1) / w4::tc::kOut * row_tiles;
-    p.split = w4::split_of(tiles, (K + w4::kUnit - 1) / w4::kUnit, wide ? sms : 2 * sms);
+    const int units = (K + w4::kUnit - 1) / w4::kUnit;
+    p.split = w4::split_of(static_cast<int64_t>((N - 1) / w4::tc::kOut + 1) * row_tiles, units, wide ? sms : 2 * sms);
+    // Two tiles of outputs to a CTA where the work fills the GPU without a split and few sums
+    // are drained: 389 rows of 7168 x 5120 take 43.9 us against 48.5, 1024 rows of 12288 x 4096
+    // 112 against 129; with a split 64 rows of 4096 x 4096 take 21.0 against 9.7; at group 32
+    // (389 rows) 101 against 76.
+    const int64_t pairs = static_cast<int64_t>((N - 1) / (2 * w4::tc::kOut) + 1) * row_tiles;
+    const bool pair = wide && group == 128 && w4::split_of(pairs, units, sms) == 1;
+    if (pair) p.split = 1;
     CUtensorMap xm;
     if (!encode_tmap_bytes(&w, codes, K / 2, N, w4::tc::kOut, 64) ||
         !encode_tmap_bf16_sw128(&xm, x, K, R, static_cast<uint64_t>(K) * 2, 64, p.tile_n))
       return SPADE_ERR_CUDA;
-    if (wide)
-      e = group == 128 ? w4::rows<128, true>(p, w, xm, s)
-          : group == 64 ? w4::rows<64, true>(p, w, xm, s)
-                        : w4::rows<32, true>(p, w, xm, s);
+    if (pair)
+      e = w4::rows<128, true, 2>(p, w, xm, s);
+    else if (wide)
+      e = group == 128 ? w4::rows<128, true, 1>(p, w, xm, s)
+          : group == 64 ? w4::rows<64, true, 1>(p, w, xm, s)
+                        : w4::rows<32, true, 1>(p, w, xm, s);
     else
-      e = group == 128 ? w4::rows<128, false>(p, w, xm, s)
-          : group == 64 ? w4::rows<64, false>(p, w, xm, s)
-                        : w4::rows<32, false>(p, w, xm, s);
+      e = group == 128 ? w4::rows<128, false, 1>(p, w, xm, s)
+          : group == 64 ? w4::rows<64, false, 1>(p, w, xm, s)
+                        : w4::rows<32, false, 1>(p, w, xm, s);
   }
   return e == cudaSuccess ? SPADE_OK : cuda_fail(e, "linear_w4 launch");
 }

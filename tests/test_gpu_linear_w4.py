@@ -60,6 +60,13 @@ def test_sizes(dev, R, N, K, group):
     _check(*_run(dev, R, N, K, group, N % 2 == 0))
 
 
+@pytest.mark.parametrize("R,N,K,group", [(5, 20000, 4352, 32), (8, 19600, 2304, 64), (1, 40000, 512, 128), (3, 41, 4224, 128),
+                                         (700, 5000, 1024, 128), (64, 39000, 256, 128), (200, 39000, 256, 64)])
+def test_many_tiles(dev, R, N, K, group):
+    """More outputs than one pass of the SMs holds sums for; tiles of outputs in pairs."""
+    _check(*_run(dev, R, N, K, group, R % 2 == 0))
+
+
 @pytest.mark.parametrize("R", [4, 40])
 def test_residual_is_the_output(dev, R):
     _check(*_run(dev, R, 321, 256, 64, True, in_place=True))

@@ -64,14 +64,14 @@ SPADE_DEVICE float divided(float x, float s, float y) {
 
 // Group of 64 dims (eight lanes): the lane's code word and the group's pair.
 SPADE_DEVICE void quantise(const float (&x)[8], uint32_t &codes, uint32_t &pair) {
-  float lo = 0.f, hi = 0.f;
-  bool finite = true;
+  float lo = 0.f, hi = 0.f, none = 0.f;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    lo = fminf(lo, x[e]);
-    hi = fmaxf(hi, x[e]);
-    finite = finite && fabsf(x[e]) <= FLT_MAX;
+  for (int e = 0; e < 8; e += 2) {
+    lo = min3(lo, x[e], x[e + 1]);
+    hi = max3(hi, x[e], x[e + 1]);
+    none = __fmaf_rn(x[e], 0.f, __fmaf_rn(x[e + 1], 0.f, none));  // NaN for an infinity or a NaN
   }
+  const bool finite = none == 0.f;
 #pragma unroll
   for (int o = 1; o < 8; o *= 2) {
     lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
@@ -85,13 +85,13 @@ SPADE_DEVICE void quantise(const float (&x)[8], uint32_t &codes, uint32_t &pair)
   const float y = __frcp_rn(real ? s : 1.f);
   constexpr float kWhole = 12582912.f;  // 1.5 2^23: adding it rounds to a whole number, ties to even
   const float z = real ? fminf(divided(-lo, s, y) + kWhole - kWhole, 15.f) : 0.f;
-  uint32_t w = 0;
+  // A quotient within -z .. 15 - z rounds to within them (they are whole), and the fields'
+  // sum needs no mask: kWhole's bits and z go in and out of all eight at once.
+  uint32_t w = static_cast<uint32_t>(static_cast<int>(z)) * 0x11111111u - 0x11111111u * __float_as_uint(kWhole);
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    // (A scale that was cut leaves quotients of any size.)
-    const float q = fminf(fmaxf(divided(x[e], s, y), -64.f), 64.f);
-    const int c = __float_as_int(q + kWhole) - __float_as_int(kWhole) + static_cast<int>(z);
-    w |= static_cast<uint32_t>(min(max(c, 0), 15)) << (4 * ((e >> 1) + 4 * (e & 1)));
+    const float q = fminf(fmaxf(divided(x[e], s, y), -z), 15.f - z);
+    w += __float_as_uint(q + kWhole) << (4 * ((e >> 1) + 4 * (e & 1)));
   }
   codes = real ? w : 0u;
   const __half2 h = __halves2half2(vote == 0xffu ? hs : __ushort_as_half(0x7fff), __float2half_rn(z));

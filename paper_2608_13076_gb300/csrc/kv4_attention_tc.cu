@@ -72,7 +72,7 @@ constexpr uint32_t kColS = 0, kColO = 256, kColK = 320;
 // scores' buffer is free once the weights are written, which PV(j-2) waited for.  No
 // phase can run two ahead of a waiter: each next one needs the waiter's own next arrival.
 constexpr int kBarFull = 0, kBarEmpty = 4, kBarKFull = 8, kBarSDone = 10, kBarVFull = 12, kBarPVDone = 14,
-              kBarPFull = 16, kBarScale = 18, kBarSeg = 22, kBarQ = 23, kBarDrain = 24, kNumBars = 25;
+              kBarPFull = 16, kBarScale = 18, kBarQ = 22, kBarDrain = 23, kNumBars = 24;
 
 struct Smem {
   static constexpr int RING = 0;
@@ -169,7 +169,6 @@ __global__ void __launch_bounds__(kThreads, 1)
         mbar_init(&bars[kBarPFull + s], kSoftWarps);
       }
       for (int s = 0; s < kScaleSlots; ++s) mbar_init(&bars[kBarScale + s], 4);
-      mbar_init(&bars[kBarSeg], kSoftWarps);
       mbar_init(&bars[kBarQ], kSoftWarps);
       mbar_init(&bars[kBarDrain], 1);
       fence_mbar_init();
@@ -290,17 +289,15 @@ __global__ void __launch_bounds__(kThreads, 1)
     const bool leader = elect_one();
     bool ok = true;
     uint32_t it = 0, seg = 0;
-    // (The flag is looked at once per chunk.)
     auto wait = [&](int bar, uint32_t parity) {
       ok = __all_sync(0xffffffffu, mbar_wait_lean(&bars[bar], parity, s_abort)) && ok;
     };
     auto issue_pv = [&](uint32_t j, bool first) {
       const int st = j % kStages;
       const uint32_t ph = (j / kStages) & 1;
-      wait(kBarVFull + st, ph);
-      wait(kBarPFull + st, ph);
-      // The segment's first PV overwrites O^T: the previous epilogue has read it.
-      if (first) wait(kBarSeg, seg & 1);
+      // (A segment's first weights come after the epilogue of the one before has read O^T.)
+      ok = __all_sync(0xffffffffu, mbar_wait_lean(&bars[kBarVFull + st], ph, s_abort) &&
+                                       mbar_wait_lean(&bars[kBarPFull + st], ph, s_abort)) && ok;
       tc_fence_after();
       const uint64_t dv = desc_sw128(smem_base + Smem::V + st * kTile, kSlab, 1024);
       const uint64_t dp = desc_sw128(smem_base + Smem::P + st * kPBytes, kSlab, 1024);
@@ -310,12 +307,12 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (leader) tc_commit(&bars[kBarPVDone + st]);
     };
     bool before_first = false;  // whether the chunk before was the first of its segment
-    while (!__any_sync(0xffffffffu, *s_abort != 0)) {
+    for (;;) {
       const int st = it % kStages;
       const uint32_t ph = (it / kStages) & 1;
       wait(kBarKFull + st, ph);
       if (!ok) break;
-      const int flags = uniform(s_cmeta[it % kScaleSlots]);
+      const int flags = s_cmeta[it % kScaleSlots];
       if (flags & kEnd) break;
       const bool first = flags & kFirst;
       // The segment's Q is staged: its S products may start while the previous
@@ -360,7 +357,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int rs = it % kRing, st = it % kStages;
       const uint32_t ph = (it / kStages) & 1;
       const uint8_t *stage = smem + Smem::RING + rs * kStage;
-      ok = *s_abort == 0 && mbar_wait_lean(&bars[kBarFull + rs], (it / kRing) & 1, s_abort) &&
+      ok = mbar_wait_lean(&bars[kBarFull + rs], (it / kRing) & 1, s_abort) &&
            mbar_wait_lean(&bars[(is_v ? kBarPVDone : kBarSDone) + st], ph ^ 1, s_abort);
       if (!__all_sync(0xffffffffu, ok)) {
         ok = false;
@@ -481,10 +478,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       fence_proxy_async_smem();
       named_bar(1, kSoftThreads);
       __syncwarp();
-      if (lane == 0) {
-        if (seg == 0) mbar_arrive(&bars[kBarQ]);
-        mbar_arrive(&bars[kBarSeg]);
-      }
+      if (lane == 0 && seg == 0) mbar_arrive(&bars[kBarQ]);
       SegInfo si_next = si;
       si_next.n_here = 0;
       if (si.seg_end < x_end) {
@@ -510,7 +504,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 
         // Scores of this key lane relative to `off` (one per row), in log2 units: the groups'
         // sums under their scales.
-        expired = expired || *s_abort || !mbar_wait_lean(&bars[kBarScale + it % kScaleSlots], (it / kScaleSlots) & 1, s_abort);
+        expired = expired || !mbar_wait_lean(&bars[kBarScale + it % kScaleSlots], (it / kScaleSlots) & 1, s_abort);
         const float2 sk = s_scale[(it % kScaleSlots) * kKeys + t];
         auto load_scores = [&](const float *off) {
 #pragma unroll

@@ -23,10 +23,10 @@
 //    issues the MMAs, warps 2-9 run the softmax and the epilogue, warps 10-13 unpack
 //    keys, warps 14-17 values (96 registers a thread; the merge takes two rows at a
 //    time to stay within them).
-//  * Bound, at few rows, by the copies (4 KB boxes take an SM's copy engine 340 cycles
-//    each, four to 128 keys), at many by the softmax warps' instructions: 64 sequences of
-//    0 to 8191 keys, 40 heads over 8, one row each, 108 us; four of 32768, 64 heads over 8, five
-//    rows each, 64 us.  The same in bf16 reads 3.6 times the bytes.
+//  * Bound, at few rows, by a chunk's chain of latencies (copy, unpack, MMA, softmax, MMA
+//    over two-stage buffers: 1900 cycles per 128 keys), at many by the softmax warps'
+//    instructions (2500): 64 sequences of 0 to 8192 keys, 40 heads over 8, one row each,
+//    108 us; four of 32768, 64 heads over 8, five rows each, 64 us.
 //  * Slots that no row may see get P = 0 by their index and zero values, whatever
 //    their scales hold.  A scale that is not finite in a slot that is seen (of the
 //    key or the value) turns the slot's score into NaN and its values into zeros, so

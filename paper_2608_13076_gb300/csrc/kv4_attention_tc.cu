@@ -24,9 +24,9 @@
 //    keys, warps 14-17 values (96 registers a thread; the merge takes two rows at a
 //    time to stay within them).
 //  * Bound, at few rows, by a chunk's chain of latencies (copy, unpack, MMA, softmax, MMA
-//    over two-stage buffers: 1900 cycles per 128 keys), at many by the softmax warps'
+//    over two-stage buffers: 1800 cycles per 128 keys), at many by the softmax warps'
 //    instructions (2500): 64 sequences of 0 to 8192 keys, 40 heads over 8, one row each,
-//    108 us; four of 32768, 64 heads over 8, five rows each, 64 us.
+//    102 us; four of 32768, 64 heads over 8, five rows each, 64 us.
 //  * Slots that no row may see get P = 0 by their index and zero values, whatever
 //    their scales hold.  A scale that is not finite in a slot that is seen (of the
 //    key or the value) turns the slot's score into NaN and its values into zeros, so
@@ -246,12 +246,20 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (n_here == 0) break;
       const int b = uniform(si.g.b), kvh = uniform(si.g.kvh);
       const int live = s_ctx[b] + s_kd[b] + 1;  // live slots of the sequence
+      // Each slice lies in one page; the lanes look up 32 slices at once, one batch ahead (a
+      // lookup per chunk held this warp for 600 cycles of its 1900).
+      auto rows_of = [&](int slice) {
+        return slice + lane < n_here ? paged_row(p, b, kvh, (ci + slice + lane) * kChunk) : 0;
+      };
+      int rows = rows_of(0), rows_next = 0;
       for (int c = 0; c < nchunk; ++c) {
         const int nsl = min(2, n_here - 2 * c);
         const int key0 = (ci + 2 * c) * kChunk;
-        // Each slice lies in one page, found before the stage's wait.
-        const int row_a = uniform(paged_row(p, b, kvh, key0));
-        const int row_b = nsl == 2 ? uniform(paged_row(p, b, kvh, key0 + kChunk)) : 0;
+        if (c % 16 == 0) {
+          if (c) rows = rows_next;
+          rows_next = rows_of(2 * c + 32);
+        }
+        const int row_a = __shfl_sync(0xffffffffu, rows, 2 * c % 32), row_b = __shfl_sync(0xffffffffu, rows, (2 * c + 1) % 32);
         uint8_t *stage = smem + Smem::RING + st * kStage;
         ok = warp_wait(&bars[kBarEmpty + st], ph, s_abort);
         if (!ok) break;

@@ -245,8 +245,8 @@ __global__ void __launch_bounds__(kThreads, 1) few_rows_kernel(const __grid_cons
 // since halving the unpacking is worth more (389 rows of 7168 x 5120 in tiles of 56 rows, two
 // CTAs: 99 us).  At group 128 a CTA can take two tiles of outputs: they share the copies of x
 // and a CTA's start and end, with three blocks of sums and two of unpacked weights in turn.
-// 20 rows of 8192 x 8192, group 64: 16.1 us; 389 rows of 7168 x 5120, group 128: 43.9 us, and
-// 1024 rows of 12288 x 4096: 112 us (650 and 920 TFLOP/s).
+// 20 rows of 8192 x 8192, group 64: 16.1 us; 389 rows of 7168 x 5120, group 128: 39.8 us, and
+// 1024 rows of 12288 x 4096: 112 us (720 and 920 TFLOP/s).
 // Where the tiles do not fill the GPU, a cluster of 2, 4 or 8 CTAs takes a tile's units
 // in equal parts and adds the sums through distributed shared memory in a fixed order.
 namespace tc {
@@ -621,19 +621,19 @@ static cudaError_t rows(const Params &p, const CUtensorMap &w, const CUtensorMap
   return launch(tc::rows_kernel<G, kWide, kTiles>, grid, p.split, S::kThreads, S::kBytes, s, p, w, x);
 }
 
-// CTAs that share a tile's units, of at least four each: those that finish first, when a
-// CTA takes as long as its units and 8 more (its start, its first copies, its sums), and
-// the GPU has `slots` of them at a time; the fewer the better.
-static int split_of(int64_t tiles, int units, int slots) {
+// How the work is dealt out: CTAs that share a tile's units, and what the slowest of
+// `slots` CTAs at a time then takes, in units of one: its units and eight more (its start, its
+// first copies, its sums).
+struct Deal {
+  int split;
+  int64_t cost;
+};
+static Deal deal(int64_t tiles, int units, int slots) {
   constexpr int kFixed = 8;
-  int best = 1;
-  int64_t cost = INT64_MAX;
-  for (int s = 1; s <= tc::kMaxSplit && (s == 1 || units >= 4 * s); s *= 2) {
+  Deal best = {1, INT64_MAX};
+  for (int s = 1; s <= tc::kMaxSplit && (s == 1 || units >= 4 * s); s *= 2) {  // (four units each at least)
     const int64_t c = ((tiles * s - 1) / slots + 1) * ((units - 1) / s + 1 + kFixed);
-    if (c < cost) {
-      cost = c;
-      best = s;
-    }
+    if (c < best.cost) best = {s, c};
   }
   return best;
 }
@@ -675,19 +675,33 @@ extern "C" spade_status spade_linear_w4(const void *x, const void *codes, const 
   } else {
     const bool wide = R > w4::tc::kNarrow;
     const int most = wide ? w4::tc::kMost : w4::tc::kNarrow;
-    const int row_tiles = (R - 1) / most + 1;
+    int row_tiles = (R - 1) / most + 1;
     if (row_tiles > 65535) return fail(SPADE_ERR_SHAPE, "spade_linear_w4: R = %d exceeds %d rows per call", R, 65535 * most);
-    p.tile_rows = (R - 1) / row_tiles + 1;
-    p.tile_n = (p.tile_rows + 15) / 16 * 16;
-    const int units = (K + w4::kUnit - 1) / w4::kUnit;
-    p.split = w4::split_of(static_cast<int64_t>((N - 1) / w4::tc::kOut + 1) * row_tiles, units, wide ? sms : 2 * sms);
+    const int units = (K + w4::kUnit - 1) / w4::kUnit, slots = wide ? sms : 2 * sms;
+    const int64_t outs = (N - 1) / w4::tc::kOut + 1, pairs = (N - 1) / (2 * w4::tc::kOut) + 1;
     // Two tiles of outputs to a CTA where the work fills the GPU without a split and few sums
-    // are drained: 389 rows of 7168 x 5120 take 43.9 us against 48.5, 1024 rows of 12288 x 4096
+    // are drained: 389 rows of 7168 x 5120 (in four tiles of rows) take 43.9 us against 48.5, 1024 rows of 12288 x 4096
     // 112 against 129; with a split 64 rows of 4096 x 4096 take 21.0 against 9.7; at group 32
     // (389 rows) 101 against 76.
-    const int64_t pairs = static_cast<int64_t>((N - 1) / (2 * w4::tc::kOut) + 1) * row_tiles;
-    const bool pair = wide && group == 128 && w4::split_of(pairs, units, sms) == 1;
-    if (pair) p.split = 1;
+    const bool pair = wide && group == 128 && w4::deal(pairs * row_tiles, units, sms).split == 1;
+    if (wide) {
+      // More row tiles than the fewest where SMs would idle: a unit takes as long as 300
+      // rows' worth of its own and its rows (rounded up to 16).  The 389 rows in five
+      // tiles of 80: 39.8 us against 43.5.
+      const int fewest = row_tiles;
+      int64_t cost = INT64_MAX;
+      for (int t = fewest; t <= fewest + 2 && t <= 65535; ++t) {
+        const w4::Deal d = w4::deal((pair ? pairs : outs) * t, units, slots);
+        const int64_t c = d.cost * (300 + ((R - 1) / t + 16) / 16 * 16);
+        if (c < cost && (!pair || d.split == 1)) {
+          cost = c;
+          row_tiles = t;
+        }
+      }
+    }
+    p.tile_rows = (R - 1) / row_tiles + 1;
+    p.tile_n = (p.tile_rows + 15) / 16 * 16;
+    p.split = pair ? 1 : w4::deal(outs * row_tiles, units, slots).split;
     CUtensorMap xm;
     if (!encode_tmap_bytes(&w, codes, K / 2, N, w4::tc::kOut, 64) ||
         !encode_tmap_bf16_sw128(&xm, x, K, R, static_cast<uint64_t>(K) * 2, 64, p.tile_n))

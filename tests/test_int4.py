@@ -66,7 +66,7 @@ def test_quantize_is_a_rounding():
 
 
 def test_a_wrong_rounding_is_seen():
-    """The checker of cached numbers catches a code, a zero or a scale that is one step off."""
+    """The comparison of cached numbers catches a code, a zero or a scale that is one step off."""
     x = torch.randn((8, 64), generator=torch.Generator().manual_seed(5))
     codes, params = int4.quantize(x, 64)
     xd, e = x.double().numpy(), np.zeros(x.shape)

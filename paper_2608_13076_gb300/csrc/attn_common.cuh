@@ -57,6 +57,18 @@ __device__ __forceinline__ int paged_row(const Params &p, int b, int kvh, int ke
 
 constexpr int round_up_c(int x, int a) { return (x + a - 1) / a * a; }
 
+// Refuses sizes whose rows or units the kernels' 32-bit numbers do not hold: a KV head has
+// G (max_k + 1) rows, a mask multiplies G by positions up to two slices past the last, and there
+// are B * Hkv units per row block.
+inline spade_status check_rows(const char *name, int B, int Hkv, int G, int max_k) {
+  const int64_t positions = static_cast<int64_t>(max_k) + 1;
+  const int64_t blocks = (G * positions + kRowBlock - 1) / kRowBlock, heads = static_cast<int64_t>(B) * Hkv;
+  if (G * (positions + 2 * kChunk) > INT32_MAX || heads > INT32_MAX || heads * blocks > INT32_MAX)
+    return fail(SPADE_ERR_CAPACITY, "%s: max_k = %d with %d query heads per KV head and %d x %d KV heads exceeds 2^31 rows",
+                name, max_k, G, B, Hkv);
+  return SPADE_OK;
+}
+
 // n / d for n >= 0, d > 0: a 32-bit division whenever both fit (every schedule
 // of practical size), else the 64-bit one.  A 64-bit division is a long
 // software sequence, and the schedule sits on the path to the first copy.

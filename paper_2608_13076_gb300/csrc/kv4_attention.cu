@@ -31,18 +31,20 @@ extern "C" spade_status spade_verify_attention_kv4(
     return fail(SPADE_ERR_CAPACITY, "%s: max_pages * page_size exceeds 2^31", name);
   if (static_cast<int64_t>(num_pages) * Hkv * page_size >= (int64_t(1) << 31))
     return fail(SPADE_ERR_CAPACITY, "%s: pool rows (pages * Hkv * page_size) exceed 2^31", name);
+  const int G = Hq / Hkv;
+  spade_status st = attn::check_rows(name, B, Hkv, G, max_k);
+  if (st != SPADE_OK) return st;
   if (!aligned(q, 16) || !aligned(out, 16) || !aligned(k_codes, 16) || !aligned(k_params, 16) || !aligned(v_codes, 16) ||
       !aligned(v_params, 16))
     return fail(SPADE_ERR_INVALID_ARG, "%s: q, pools and out must be 16-byte aligned", name);
   int sms = 0;
-  spade_status st = device_info(&sms, nullptr);
+  st = device_info(&sms, nullptr);
   if (st != SPADE_OK) return st;
   const int cap = max_pages * page_size;
   const size_t need = spade_attn_workspace_size(B, Hq, Hkv, D, cap, max_k);
   if (!workspace || workspace_bytes < need || !aligned(workspace, 256))
     return fail(SPADE_ERR_WORKSPACE, "%s: workspace needs %zu bytes, 256-byte aligned (got %zu)", name, need,
                 workspace_bytes);
-  const int G = Hq / Hkv;
   const int RB = (G * (max_k + 1) + attn::kRowBlock - 1) / attn::kRowBlock;
   const int units = B * Hkv * RB;
 

@@ -509,8 +509,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int key0 = (g.ci + 2 * c) * kChunk;
         const int nk = min(2, si.n_here - 2 * c) * kChunk;
         const int kg = key0 + t;
-        // Row R = 64 rb + rr (position R / G) sees key kg iff R >= (kg - ctx) G.
-        const int lo = (t < nk) ? (kg - ctx) * p.G - kRowBlock * g.rb - c0 : NH;
+        // Row R = 64 rb + rr (position R / G) sees key kg iff R >= (kg - ctx) G (every row where
+        // kg <= ctx: far behind it the product would pass 32 bits).
+        const int lo = (t < nk) ? max(kg - ctx, 0) * p.G - kRowBlock * g.rb - c0 : NH;
         const bool masked = __any_sync(0xffffffffu, lo > 0);  // (the last keys of a sequence or segment)
         const uint32_t taddr = tlane + kColS + st * NG * 64 + c0;
 

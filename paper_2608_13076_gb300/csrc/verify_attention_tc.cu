@@ -412,9 +412,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int key0 = (g.ci + 2 * c) * kChunk;  // first key of the chunk (sequence position)
         const int nk = min(2, si.n_here - 2 * c) * kChunk;
         const int kg = key0 + t;
-        // Row R = 64 rb + rr (position R / G) sees key kg iff R >= (kg - ctx) G:
-        // the visible rows of this key lane are rr in [lo, nrow).
-        const int lo = (t < nk) ? max(0, (kg - ctx) * p.G - kRowBlock * g.rb) - c0 : NH;
+        // Row R = 64 rb + rr (position R / G) sees key kg iff R >= (kg - ctx) G (every row
+        // where kg <= ctx: far behind it the product would pass 32 bits): the visible rows
+        // of this key lane are rr in [lo, nrow).
+        const int lo = (t < nk) ? max(0, max(kg - ctx, 0) * p.G - kRowBlock * g.rb) - c0 : NH;
         const uint32_t taddr = tlane + kColS + st * 64 + c0;
 
         // ---- S^T lane t, this warp's rows: scale, mask, test vs maxima ----

@@ -402,6 +402,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           tmem_st16(tmem + (static_cast<uint32_t>(q4 * 32) << 16) + kColK + st * (D / 2) + j * 16, a);
         }
         // The scales that the scores take, in log2 units: NaN where the key's or the value's is not finite.
+        // (One group: the second stays 0, see the scores.)
         float2 s = make_float2(0.f, 0.f);
         const float poison = finite ? p.scale_log2 : NAN;
         s.x = (finite_scale(kp[0]) ? int4::pair_of(kp[0]).x : NAN) * poison;
@@ -537,11 +538,16 @@ __global__ void __launch_bounds__(kThreads, 1)
               for (int e = 0; e < 4; e += 2) {
                 // -m = inf (no visible key yet) gives inf for a visible score: a vote.
                 // (The score is rounded before the maximum is taken off, as where it was found:
-                // the largest one's weight is 2^kPBias whatever the scores' size.)
-                F2 s = f2_mul(f2(__uint_as_float(y[0][j + e]), __uint_as_float(y[0][j + e + 1])), f2(sk.x, sk.x));
+                // the largest one's weight is 2^kPBias whatever the scores' size.  With one group
+                // the product is taken as a sum with 0, sk.y, which keeps it apart from the sum
+                // that follows: fused, scores past 2^28 gave weights past float16.)
+                const F2 s0 = f2(__uint_as_float(y[0][j + e]), __uint_as_float(y[0][j + e + 1])), k0 = f2(sk.x, sk.x);
+                F2 s;
                 if constexpr (NG == 2)
                   s = f2_fma(f2(__uint_as_float(y[NG - 1][j + e]), __uint_as_float(y[NG - 1][j + e + 1])),
-                             f2(sk.y, sk.y), s);
+                             f2(sk.y, sk.y), f2_mul(s0, k0));
+                else
+                  s = f2_fma(s0, k0, f2(sk.y, sk.y));
                 s = f2_add(s, e ? f2(mv.z, mv.w) : f2(mv.x, mv.y));
                 f2_split(s, x_[r0 + j + e], x_[r0 + j + e + 1]);
               }

@@ -39,7 +39,9 @@ SPADE_DEVICE uint32_t and_or(uint32_t a, uint32_t mask, uint32_t bits) {
 }
 
 // ---------------------------------------------------------------- fp32 pairs
-// Two fp32 operations per instruction, each rounded as its scalar form.
+// Two fp32 operations per instruction.  A product that is added to something may become
+// one fused operation, although both ask for a rounding (as measured; a sum after f2_fma
+// is rounded apart): no result may depend on the product's own rounding.
 struct F2 {
   uint64_t v;
 };

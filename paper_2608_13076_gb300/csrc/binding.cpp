@@ -74,7 +74,13 @@ const at::Tensor &u8(PyObject *o, const char *name) { return need(o, name, Scala
 const int32_t *ip(const at::Tensor &t) { return static_cast<const int32_t *>(t.data_ptr()); }
 int32_t *ip_mut(const at::Tensor &t) { return static_cast<int32_t *>(t.data_ptr()); }
 const float *fp(const at::Tensor *t) { return t ? static_cast<const float *>(t->data_ptr()) : nullptr; }
-int32_t n32(int64_t v) { return static_cast<int32_t>(v); }
+// A size or bound that the library's 32-bit arguments do not hold (thrown without the
+// interpreter lock, so the exception is set by `guarded`).
+struct TooLarge {};
+int32_t n32(int64_t v) {
+  if (v < INT32_MIN || v > INT32_MAX) throw TooLarge{};
+  return static_cast<int32_t>(v);
+}
 
 int32_t as_int(PyObject *o) {
   PyObject *n = PyNumber_Long(o);
@@ -82,7 +88,7 @@ int32_t as_int(PyObject *o) {
   const long long v = PyLong_AsLongLong(n);
   Py_DECREF(n);
   if (v == -1 && PyErr_Occurred()) throw Bad{};
-  return static_cast<int32_t>(v);
+  return n32(v);
 }
 float as_float(PyObject *o) {
   const double v = PyFloat_AsDouble(o);
@@ -118,6 +124,9 @@ PyObject *guarded(Py_ssize_t n, Py_ssize_t want, F f) {
   try {
     return PyLong_FromLong(static_cast<long>(f()));
   } catch (const Bad &) {
+    return nullptr;
+  } catch (const TooLarge &) {
+    PyErr_SetString(PyExc_ValueError, "a size or bound does not fit 32 bits (2^31 - 1 at most)");
     return nullptr;
   } catch (const std::exception &e) {
     PyErr_SetString(PyExc_RuntimeError, e.what());

@@ -88,7 +88,7 @@ __global__ void __launch_bounds__(kThreads, 1) few_rows_kernel(const __grid_cons
   extern __shared__ __align__(16) uint8_t smem[];
   const int warp = uniform_warp(), lane = threadIdx.x & 31;
   const int r = lane >> 2, t = lane & 3;
-  const int groups = p.K / G, spans = (p.K + kSpan - 1) / kSpan, row_bytes = p.K / 2;
+  const int groups = p.K / G, spans = (p.K - 1) / kSpan + 1, row_bytes = p.K / 2;
   uint8_t *ring = smem + warp * kRing * F::kStage;
   float4 *sums = reinterpret_cast<float4 *>(smem + F::kRings);
   // Warps along K (a power of two) and along the tiles.
@@ -601,7 +601,7 @@ static cudaError_t few_rows(Params p, int sms, cudaStream_t s) {
   static OncePerDevice once;
   const cudaError_t e = set_max_smem(once, F::kRings + kHold * F::kSums, few_rows_kernel<G>);
   if (e != cudaSuccess) return e;
-  const int tiles = (p.N - 1) / kTile + 1, spans = (p.K + kSpan - 1) / kSpan;
+  const int tiles = (p.N - 1) / kTile + 1, spans = (p.K - 1) / kSpan + 1;
   const int grid = tiles < sms ? tiles : sms, most = (tiles - 1) / grid + 1;  // tiles of a CTA
   // Warps along K: as many as have a span; with a single tile all of them share it anyway.
   p.split = kWarps;
@@ -677,7 +677,7 @@ extern "C" spade_status spade_linear_w4(const void *x, const void *codes, const 
     const int most = wide ? w4::tc::kMost : w4::tc::kNarrow;
     int row_tiles = (R - 1) / most + 1;
     if (row_tiles > 65535) return fail(SPADE_ERR_SHAPE, "spade_linear_w4: R = %d exceeds %d rows per call", R, 65535 * most);
-    const int units = (K + w4::kUnit - 1) / w4::kUnit, slots = wide ? sms : 2 * sms;
+    const int units = (K - 1) / w4::kUnit + 1, slots = wide ? sms : 2 * sms;
     const int64_t outs = (N - 1) / w4::tc::kOut + 1, pairs = (N - 1) / (2 * w4::tc::kOut) + 1;
     // Two tiles of outputs to a CTA where the work fills the GPU without a split and few sums
     // are drained: 389 rows of 7168 x 5120 (in four tiles of rows) take 43.9 us against 48.5, 1024 rows of 12288 x 4096

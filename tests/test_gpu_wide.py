@@ -30,3 +30,19 @@ def test_bound_past_32_bits(dev, max_k):
     ws = torch.zeros(1 << 24, dtype=torch.uint8, device=dev)
     with pytest.raises((ValueError, OverflowError)):
         C.attention(c, q, max_k=max_k, workspace=ws)
+
+
+@pytest.mark.parametrize("R", [1, 9])
+def test_projection_of_nearly_2_31_columns(dev, R):
+    """The most columns that an int32 holds in whole groups: the first, a middle and the last one count, the
+    others are zeros (an exact sum, worked by hand)."""
+    K = 2**31 - 64
+    x = torch.zeros((R, K), dtype=torch.bfloat16, device=dev)
+    for at, v in ((0, 1.0), (K // 2 + 5, 2.0), (K - 1, 4.0)):
+        x[:, at] = v
+    codes = torch.full((1, K // 2), 0x33, dtype=torch.uint8, device=dev)  # 3 - 1 everywhere
+    params = torch.ones((1, K // 64, 2), dtype=torch.float16, device=dev)
+    out, st = torch.zeros((R, 1), dtype=torch.bfloat16, device=dev), spade.status_tensor(dev)
+    spade.spade_linear_w4(x, codes, params, out, status=st)
+    torch.cuda.synchronize()
+    assert int(st.item()) == 0 and (out == 14).all()

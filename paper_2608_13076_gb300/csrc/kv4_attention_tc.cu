@@ -288,10 +288,13 @@ __global__ void __launch_bounds__(kThreads, 1)
       s_rmeta[st] = make_int2(0, kEnd);
       mbar_arrive(&bars[kBarFull + st]);
     }
-    if (!ok && leader) {
-      atomicOr(p.status, SPADE_DEV_TIMEOUT);
-      // Drain: every copy issued must land before the CTA's smem goes away.
-      for (uint32_t j = (issued > kRing ? issued - kRing : 0); j < issued; ++j)
+    if (leader) {
+      if (!ok) atomicOr(p.status, SPADE_DEV_TIMEOUT);
+      // Every copy issued must land before the CTA's shared memory goes away, also where
+      // another warp's wait expires once this one is done (else all have: the unpacking warps
+      // waited for them).  The stage of kEnd was waited for above.
+      const uint32_t left = ok ? kRing - 1 : kRing;
+      for (uint32_t j = issued > left ? issued - left : 0; j < issued; ++j)
         mbar_wait_unabortable(&bars[kBarFull + j % kRing], (j / kRing) & 1);
     }
   } else if (warp == 1) {
@@ -353,8 +356,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       before_first = first;
       ++it;
     }
-    if (leader && (!ok || *s_abort)) {
-      atomicOr(p.status, SPADE_DEV_TIMEOUT);
+    if (leader) {
+      if (!ok || *s_abort) atomicOr(p.status, SPADE_DEV_TIMEOUT);
+      // Every MMA issued must be done before its operands and the tensor memory go away.
       tc_commit(&bars[kBarDrain]);
       mbar_wait_unabortable(&bars[kBarDrain], 0);
     }

@@ -392,7 +392,9 @@ __global__ void __launch_bounds__(Shape<G, kWide, kTiles>::kThreads, Shape<G, kW
       }
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
-    if (!ok && leader)  // every copy issued must land before the CTA's shared memory goes away
+    // Every copy issued must land before the CTA's shared memory goes away, also where another
+    // warp's wait expires once this one is done (else all have: the consumers waited for them).
+    if (leader)
       for (uint32_t j = issued > S::kStages ? issued - S::kStages : 0; j < issued; ++j)
         mbar_wait_unabortable(&s_full[j % S::kStages], (j / S::kStages) & 1);
   } else if (warp == 1) {
@@ -446,8 +448,8 @@ __global__ void __launch_bounds__(Shape<G, kWide, kTiles>::kThreads, Shape<G, kW
         tc_commit(&s_empty[st]);
       }
     }
-    if (leader && (!ok || *const_cast<volatile int *>(&s_abort))) {
-      // Every MMA issued must be done before its operands and the tensor memory go away.
+    // Every MMA issued must be done before its operands and the tensor memory go away (see the copies).
+    if (leader) {
       tc_commit(&s_drain);
       mbar_wait_unabortable(&s_drain, 0);
     }

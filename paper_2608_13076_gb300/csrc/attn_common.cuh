@@ -44,9 +44,10 @@ struct Params {
 
 // Pool row of the 64-key slice starting at key `key` of (b, kvh) in a paged
 // cache.  An out-of-range page id is reported and mapped past the last row,
-// where the tensor copy reads zeros.
+// where the tensor copy reads zeros.  (A plain load: the kernels are launched while the one
+// before still runs, and a read-only load promises that nothing writes its data meanwhile.)
 __device__ __forceinline__ int paged_row(const Params &p, int b, int kvh, int key) {
-  const int page = __ldg(p.block_table + static_cast<int64_t>(b) * p.max_pages + key / p.page_size);
+  const int page = p.block_table[static_cast<int64_t>(b) * p.max_pages + key / p.page_size];
   const int64_t rows = static_cast<int64_t>(p.num_pages) * p.Hkv * p.page_size;
   if (page < 0 || page >= p.num_pages) {
     atomicOr(p.status, SPADE_DEV_BAD_INDEX);

@@ -150,7 +150,8 @@ size_t spade_qkv_workspace_size(int32_t R, int32_t Hq, int32_t Hkv, int32_t D);
  *   lse        float32 [R, Hq] natural-log sum-exp of the scaled scores, or NULL
  *   B, Hq, Hkv, D, cap, max_k, R   sizes; Hq % Hkv == 0; D in {64, 128};
  *              Hq / Hkv * (max_k + 1) query rows share each KV head (sizes whose
- *              rows pass 31 bits are refused with SPADE_ERR_CAPACITY)
+ *              rows, or the 64-slot slices of all a head's blocks of 64 rows,
+ *              pass 31 bits are refused with SPADE_ERR_CAPACITY)
  *   workspace  device scratch of at least spade_attn_workspace_size(...) bytes,
  *              256-byte aligned, ZEROED ONCE by the caller after allocation;
  *              every call that completes leaves it zeroed again.  Calls that

@@ -58,15 +58,19 @@ __device__ __forceinline__ int paged_row(const Params &p, int b, int kvh, int ke
 
 constexpr int round_up_c(int x, int a) { return (x + a - 1) / a * a; }
 
-// Refuses sizes whose rows or units the kernels' 32-bit numbers do not hold: a KV head has
-// G (max_k + 1) rows, a mask multiplies G by positions up to two slices past the last, and there
-// are B * Hkv units per row block.
-inline spade_status check_rows(const char *name, int B, int Hkv, int G, int max_k) {
+// Refuses sizes that the kernels' 32-bit numbers do not hold: a KV head has G (max_k + 1) rows, a
+// mask multiplies G by positions up to two slices past the last, there are B * Hkv units per row
+// block, and a KV head's row blocks lie end to end in the schedule, each as long as its slices of
+// at most `cap` slots and its virtual ones.
+inline spade_status check_rows(const char *name, int B, int Hkv, int G, int max_k, int cap) {
   const int64_t positions = static_cast<int64_t>(max_k) + 1;
   const int64_t blocks = (G * positions + kRowBlock - 1) / kRowBlock, heads = static_cast<int64_t>(B) * Hkv;
-  if (G * (positions + 2 * kChunk) > INT32_MAX || heads > INT32_MAX || heads * blocks > INT32_MAX)
-    return fail(SPADE_ERR_CAPACITY, "%s: max_k = %d with %d query heads per KV head and %d x %d KV heads exceeds 2^31 rows",
-                name, max_k, G, B, Hkv);
+  const int64_t slices = (static_cast<int64_t>(cap) + kChunk - 1) / kChunk + 2 * kUnitCostTc;
+  if (G * (positions + 2 * kChunk) > INT32_MAX || heads > INT32_MAX || heads * blocks > INT32_MAX ||
+      blocks * slices > INT32_MAX)
+    return fail(SPADE_ERR_CAPACITY,
+                "%s: max_k = %d with %d query heads per KV head, %d x %d KV heads and %d slots leaves 32-bit row numbers",
+                name, max_k, G, B, Hkv, cap);
   return SPADE_OK;
 }
 

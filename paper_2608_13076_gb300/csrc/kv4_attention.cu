@@ -32,7 +32,7 @@ extern "C" spade_status spade_verify_attention_kv4(
   if (static_cast<int64_t>(num_pages) * Hkv * page_size >= (int64_t(1) << 31))
     return fail(SPADE_ERR_CAPACITY, "%s: pool rows (pages * Hkv * page_size) exceed 2^31", name);
   const int G = Hq / Hkv;
-  spade_status st = attn::check_rows(name, B, Hkv, G, max_k);
+  spade_status st = attn::check_rows(name, B, Hkv, G, max_k, max_pages * page_size);
   if (st != SPADE_OK) return st;
   if (!aligned(q, 16) || !aligned(out, 16) || !aligned(k_codes, 16) || !aligned(k_params, 16) || !aligned(v_codes, 16) ||
       !aligned(v_params, 16))

@@ -24,7 +24,7 @@ extern "C" size_t spade_attn_workspace_size(int32_t B, int32_t Hq, int32_t Hkv, 
                                             int32_t cap, int32_t max_k) {
   if (B <= 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv || (D != 64 && D != 128) || cap <= 0 || max_k < 0)
     return 0;
-  if (attn::check_rows("spade_attn_workspace_size", B, Hkv, Hq / Hkv, max_k) != SPADE_OK) return 0;
+  if (attn::check_rows("spade_attn_workspace_size", B, Hkv, Hq / Hkv, max_k, cap) != SPADE_OK) return 0;
   int sms = 0;
   if (device_info(&sms, nullptr) != SPADE_OK) return 0;
   const int RB = attn::row_blocks(Hq / Hkv, max_k);
@@ -61,7 +61,7 @@ static spade_status verify_attention_impl(
   if (cache_rows >= (int64_t(1) << 31))
     return fail(SPADE_ERR_CAPACITY, "KV cache rows (B or pages) * Hkv * slots exceed 2^31");
   const int G = Hq / Hkv;
-  spade_status st = attn::check_rows("spade_verify_attention", B, Hkv, G, max_k);
+  spade_status st = attn::check_rows("spade_verify_attention", B, Hkv, G, max_k, cap);
   if (st != SPADE_OK) return st;
   if (!aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(q, 16) || !aligned(out, 16))
     return fail(SPADE_ERR_INVALID_ARG, "q, caches and out must be 16-byte aligned");
@@ -193,7 +193,7 @@ extern "C" spade_status spade_verify_attention_noalloc(
     return fail(SPADE_ERR_INVALID_ARG, "spade_verify_attention_noalloc: non-positive size");
   if (Hq % Hkv) return fail(SPADE_ERR_SHAPE, "Hq (%d) must be a multiple of Hkv (%d)", Hq, Hkv);
   if (D != 64 && D != 128) return fail(SPADE_ERR_SHAPE, "head dim %d not supported (64 or 128)", D);
-  spade_status st = attn::check_rows("spade_verify_attention_noalloc", B, Hkv, Hq / Hkv, max_k);
+  spade_status st = attn::check_rows("spade_verify_attention_noalloc", B, Hkv, Hq / Hkv, max_k, cap);
   if (st != SPADE_OK) return st;
   int dev = 0;
   st = device_info(nullptr, &dev);

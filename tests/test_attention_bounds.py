@@ -56,3 +56,27 @@ def test_no_workspace_size(lib, sizes):
 def test_others_are_not(lib, call):
     """A loose bound that 32 bits hold is not refused for its size."""
     assert call(lib, 1, 8, 2, 5000) != CAPACITY
+
+
+# A prompt of a million rows behind a million slots: a KV head's 131072 row blocks of up to 32768 slices each; and
+# the longest cache under 64 blocks.
+LONG = [(1, 64, 8, (1 << 20) - 1, 1 << 21), (1, 8, 1, 511, (1 << 31) - 64)]
+
+
+@pytest.mark.parametrize("sizes", LONG)
+def test_schedules_past_32_bits_are_refused(lib, sizes):
+    B, Hq, Hkv, max_k, cap = sizes
+    rows = (B, Hq, Hkv, 64)
+    pages = (64, (2**31 - 64) // 64 // Hkv, cap // 64)
+    assert lib.spade_verify_attention_kv4(*[P] * 11, *rows, *pages, max_k, 1 << 20, P, 1 << 62, P, None) == CAPACITY
+    assert b"max_k" in lib.spade_last_error()
+    assert lib.spade_verify_attention_paged(*[P] * 9, *rows, *pages, max_k, 1 << 20, P, 1 << 62, P, None) == CAPACITY
+    assert b"max_k" in lib.spade_last_error()
+    assert lib.spade_attn_workspace_size(*rows, cap, max_k) == 0
+    assert b"max_k" in lib.spade_last_error()
+
+
+def test_long_prompts_are_not(lib):
+    """128 thousand rows of eight heads a KV head behind four million slots."""
+    assert lib.spade_verify_attention_kv4(*[P] * 11, 1, 64, 8, 64, 64, 1 << 20, 1 << 16, (1 << 17) - 1, 1 << 17, P, 1 << 62, P,
+                                          None) != CAPACITY

@@ -88,24 +88,27 @@ def turned(x, weight, turn, eps):
 def check_quantised(x, err, packed, params):
     """Whether (codes, pairs) are a rounding of numbers x [..., D], each known to within err: the pair's scale is
     fp16(span / 15) for a span within the error, zero and codes are the nearest whole numbers but for ties that
-    the error reaches.  Returns the number of violations."""
+    the error reaches; a group with a number that is not finite has the scale NaN, and no other one has.  Returns the
+    number of violations."""
     c = codes_of(packed).reshape(x.shape[:-1] + (-1, 64)).astype(np.float64)
     x = x.reshape(c.shape)
-    e = err.reshape(c.shape).max(-1)
+    finite = np.isfinite(x).all(-1)
+    x = np.where(finite[..., None], x, 0.0)
+    e = np.where(finite, err.reshape(c.shape).max(-1), 0.0)
     s, z = params[..., 0].astype(np.float64), params[..., 1].astype(np.float64)
     lo, hi = np.minimum(x.min(-1), 0), np.maximum(x.max(-1), 0)
     span, tol = (hi - lo) / 15, 2 * e / 15 + 2.0 ** -22 * (hi - lo)
     low = np.minimum(span - tol, 4364.0).clip(min=0).astype(np.float16).astype(np.float64)
     high = np.minimum(span + tol, 4364.0).astype(np.float16).astype(np.float64)
-    bad = (s < low) | (s > high)
+    bad = ~((s >= low) & (s <= high))
     live = s > 0
     safe = np.where(live, s, 1.0)
     slack = e / safe + 2.0 ** -20 * (1 + np.abs(lo / safe))
-    bad |= live & (np.abs(z - np.clip(-lo / safe, 0, 15)) > 0.5 + slack)
-    bad |= (z != np.round(z)) | (z < 0) | (z > 15) | (~live & (z != 0))
+    bad |= live & ~(np.abs(z - np.clip(-lo / safe, 0, 15)) <= 0.5 + slack)
+    bad |= ~((z == np.round(z)) & (z >= 0) & (z <= 15)) | (~live & (z != 0))
     at = x / safe[..., None] + z[..., None]
     want = np.clip(at, 0, 15)
-    off = np.abs(c - want) > 0.5 + slack[..., None]
-    off |= ~live[..., None] & (c != 0)
-    off &= live[..., None] | (c != 0)
-    return int(bad.sum() + off.sum())
+    off = ~(np.abs(c - want) <= 0.5 + slack[..., None])
+    off = np.where(live[..., None], off, c != 0)
+    bad = np.where(finite, bad, ~np.isnan(s))
+    return int(bad.sum() + (off & finite[..., None]).sum())

@@ -70,11 +70,15 @@ class ToyVerifier:
         self.w_qkv = normal(((c.Hq + 2 * c.Hkv) * c.D, c.H), 1.0 / math.sqrt(c.H))
         self.w_o = normal((c.H, c.Hq * c.D), 1.0 / math.sqrt(c.Hq * c.D))
         self.w_lm = normal((c.V, c.H), c.logit_scale / math.sqrt(c.H))
-        self.k_cache = torch.zeros((B, c.Hkv, cap, c.D), dtype=torch.bfloat16, device=dev)
-        self.v_cache = torch.zeros_like(self.k_cache)
         self.ctx = torch.zeros(B, dtype=torch.int32, device=dev)
         self.status = status_tensor(dev)
         self.device = dev
+        self._make_cache()
+
+    def _make_cache(self):
+        c = self.cfg
+        self.k_cache = torch.zeros((self.B, c.Hkv, self.cap, c.D), dtype=torch.bfloat16, device=self.device)
+        self.v_cache = torch.zeros_like(self.k_cache)
 
     def draft_logits(self, tokens):
         """The drafter's logits after `tokens` [n]: the verifier's residual path without its
@@ -129,17 +133,19 @@ class ToyVerifierInt4(ToyVerifier):
     the query and key heads, and a paged 4-bit cache in pages of `page` slots."""
 
     def __init__(self, cfg: ToyConfig, B: int, cap: int, seed: int, device, page: int = 64, group: int = 64):
+        self.page = page
         super().__init__(cfg, B, cap, seed, device)
         c, dev = cfg, self.device
-        del self.k_cache, self.v_cache
         self.w_qkv, self.w_o = (int4.quantize(w, group) for w in (self.w_qkv, self.w_o))
         self.q_norm = torch.ones(c.D, dtype=torch.bfloat16, device=dev)
         self.k_norm = torch.ones_like(self.q_norm)
-        max_pages = -(-cap // page)
-        self.rope = int4.rope_table(c.rope_theta, c.D, max_pages * page, device=dev)
+        self.rope = int4.rope_table(c.rope_theta, c.D, self.table.shape[1] * page, device=dev)
+
+    def _make_cache(self):
         # Pages dealt to the sequences in turn, as a serving pool would end up.
-        self.pools = int4.kv4_pools(B * max_pages, c.Hkv, page, c.D, device=dev)
-        self.table = torch.arange(B * max_pages, dtype=torch.int32).reshape(max_pages, B).t().contiguous().to(dev)
+        B, max_pages = self.B, -(-self.cap // self.page)
+        self.pools = int4.kv4_pools(B * max_pages, self.cfg.Hkv, self.page, self.cfg.D, device=self.device)
+        self.table = torch.arange(B * max_pages, dtype=torch.int32).reshape(max_pages, B).t().contiguous().to(self.device)
 
     def _heads(self, x, ctx, kd, cu_q, max_k):
         """Query heads of rows x; their keys and values go into the cache at ctx + i."""
@@ -158,7 +164,7 @@ class ToyVerifierInt4(ToyVerifier):
         x = self.emb[tokens].contiguous()
         q = self._heads(x, self.ctx, kd, cu_q, max_k)
         out = torch.empty_like(q)
-        slots = self.table.shape[1] * self.pools[0].shape[2]
+        slots = self.table.shape[1] * self.page
         ws = attn_workspace(self.B, c.Hq, c.Hkv, c.D, slots, max_k, device=self.device)
         spade_verify_attention_kv4(q, *self.pools, self.table, self.ctx, kd, cu_q, out, None, max_k=max_k, workspace=ws,
                                    status=self.status)

@@ -468,8 +468,9 @@ spade_status spade_verify_qkv_rope_paged(const void *x, const void *w_qkv, const
  * hi = max(x, 0), scale = (hi - lo) / 15 rounded to float16 (at most 4364, so that
  * every value is in float16's range), zero = round(-lo / scale) cut to 15, code =
  * round(x / scale) + zero cut to 0 .. 15; a group whose scale rounds to 0 (spans
- * under 4.5e-7) is held as zeros, one that spans over 65460 is cut.  A group with a value that is not finite gets scale NaN, and with it
- * every row that attends to the slot.
+ * under 4.5e-7) is held as zeros, one that spans over 65460 is cut.  A group with
+ * a value that is not finite gets scale NaN, and with it every row that attends to
+ * the slot.
  */
 
 /*
@@ -484,7 +485,10 @@ spade_status spade_verify_qkv_rope_paged(const void *x, const void *w_qkv, const
  *   R, N, K, group   any R, N >= 1; group in {32, 64, 128}; K a multiple of group
  *   status    device int32 (SPADE_DEV_TIMEOUT)
  * Every pointer 16-byte aligned.  Products are summed in fp32 in an order that
- * depends on the sizes alone.
+ * depends on the sizes alone.  Above some hundred rows the weights' bytes no longer
+ * bound a projection and unpacking costs more than it saves: 416 rows of 7168 x 5120
+ * take 41.6 us at group 128 (75 at group 32 for 389), where spade_verify_qkv_rope takes
+ * 33 us with bf16 weights, its rotation and cache write included.
  */
 spade_status spade_linear_w4(const void *x, const void *codes, const void *params,
                              const void *residual, void *out, int32_t R, int32_t N, int32_t K,
@@ -524,6 +528,10 @@ spade_status spade_verify_qk_norm_rope_kv4(
  * hold; a slot that it sees whose key or value has a scale that is not finite makes
  * the row and its lse NaN.
  * n_draft = 0 is decoding, one token per sequence.
+ * Scores are sums of exact products in fp32.  Two numbers are rounded to float16 on
+ * the way to the output (not to the lse): a value scale * (code - zero), by 2^-11 of
+ * itself at most, and a softmax weight, by 2^-11 of itself or 2^-32 of the row's
+ * largest one.  Both stay below the output's own rounding to bf16 (2^-8).
  */
 spade_status spade_verify_attention_kv4(
     const void *q, const void *k_codes, const void *k_params, const void *v_codes,

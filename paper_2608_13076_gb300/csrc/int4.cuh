@@ -1,6 +1,8 @@
 // int4.cuh -- numbers in 4 bits as include/spade.h lays them out: value = scale *
 // (code - zero), eight codes to a 32-bit word whose fields 4p .. 4p + 3 hold numbers
-// 0, 2, 4, 6, 1, 3, 5, 7, and (scale, zero) pairs of float16 per group.
+// 0, 2, 4, 6, 1, 3, 5, 7, and (scale, zero) pairs of float16 per group.  (Codes placed so
+// that a mask picks neighbours, and turned into numbers by the low bits of a larger one, is a
+// published technique: Kim et al., "Who Says Elephants Can't Run", arXiv:2211.10017, 2022.)
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>

@@ -35,8 +35,9 @@ struct Params {
 // A warp has a ring of its own, filled by its lanes with 16-byte copies; the copies' places
 // make the fragments' reads free of bank conflicts for every group size.  Sums of a tile
 // wait in shared memory and are added over the warps in a fixed order.
-// 6 rows of 12288 x 4096, group 32: 9.9 us, 3.2 TB/s; 1 row of 57344 x 8192, group 128: 57 us,
-// 4.4 TB/s, where the copies alone take 43 us and the unpacking alone 43 us: both fill the SM.
+// 6 rows of 12288 x 4096, group 32: 10.7 us, 3.0 TB/s (9.9 where three such weights stay in L2);
+// 1 row of 57344 x 8192, group 128: 54 us, 4.6 TB/s, where the copies alone take 43 us and the
+// unpacking alone 43 us: both fill the SM.
 constexpr int kWarps = 16, kThreads = 32 * kWarps;
 constexpr int kUnit = 128;   // k per unit
 constexpr int kSpan = 256;   // k of a warp: two units
@@ -245,8 +246,8 @@ __global__ void __launch_bounds__(kThreads, 1) few_rows_kernel(const __grid_cons
 // since halving the unpacking is worth more (389 rows of 7168 x 5120 in tiles of 56 rows, two
 // CTAs: 99 us).  At group 128 a CTA can take two tiles of outputs: they share the copies of x
 // and a CTA's start and end, with three blocks of sums and two of unpacked weights in turn.
-// 20 rows of 8192 x 8192, group 64: 16.1 us; 389 rows of 7168 x 5120, group 128: 39.8 us, and
-// 1024 rows of 12288 x 4096: 112 us (720 and 920 TFLOP/s).
+// 20 rows of 8192 x 8192, group 64: 16.1 us; 389 rows of 7168 x 5120, group 128: 39.6 us, and
+// 1024 rows of 12288 x 4096: 110 us (720 and 935 TFLOP/s).
 // Where the tiles do not fill the GPU, a cluster of 2, 4 or 8 CTAs takes a tile's units
 // in equal parts and adds the sums through distributed shared memory in a fixed order.
 namespace tc {
@@ -689,7 +690,7 @@ extern "C" spade_status spade_linear_w4(const void *x, const void *codes, const 
     if (wide) {
       // More row tiles than the fewest where SMs would idle: a unit takes as long as 300
       // rows' worth of its own and its rows (rounded up to 16).  The 389 rows in five
-      // tiles of 80: 39.8 us against 43.5.
+      // tiles of 80: 39.6 us against 43.5.
       const int fewest = row_tiles;
       int64_t cost = INT64_MAX;
       for (int t = fewest; t <= fewest + 2 && t <= 65535; ++t) {

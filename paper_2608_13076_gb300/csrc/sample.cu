@@ -239,7 +239,8 @@ struct Shared {
   double reach;              // T ln(min_p)
   uint32_t count, settled;
   int cut;
-  uint64_t above;
+  int cuts[2];               // a round of histograms' boundary bin, and what is above it: by turns, as a thread late in
+  uint64_t above[2];         // reading one round's must not find the next round's
   float ch, cl, tau;         // log2(e) / T, high and low part
 };
 
@@ -818,9 +819,9 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
       const float width = fmaxf(fminf(24.f * temp, FLT_MAX), w.m - number_of(~static_cast<uint32_t>(ends))) * (1.f / kBins);
       const float scale = __fdiv_rn(1.f, width);
       bool by_value = scale > 0.f && scale <= FLT_MAX;
-      while (hi - lo > 1) {
+      for (int turn = 0; hi - lo > 1; turn ^= 1) {
         if (tid < kBins) s.hist[tid] = s.high[tid] = 0;
-        if (tid == 0) s.cut = kBins;
+        if (tid == 0) s.cuts[turn] = kBins;
         __syncthreads();
         int shift = 0;
         while ((hi - 1 - lo) >> shift >= kBins) ++shift;
@@ -862,13 +863,13 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
         uint64_t upto = above + incl;
         for (int i = 0; i < warp; ++i) upto += s.warp[i];
         if (tid < kBins && upto >= goal && upto - n < goal) {
-          s.cut = tid;
-          s.above = upto - n;
+          s.cuts[turn] = tid;
+          s.above[turn] = upto - n;
         }
         cluster_sync();  // (the bins have been read by all)
-        const int cut = s.cut;
+        const int cut = s.cuts[turn];
         if (cut == kBins) return lo;
-        above = s.above;
+        above = s.above[turn];
         const uint32_t top = cut ? top_of(cut) + 1 : hi;
         if (by_value ? cut < kBins - 1 : static_cast<uint64_t>(cut + 1) << shift <= hi - 1 - lo) lo = max(lo, top_of(cut + 1) + 1);
         hi = min(hi, top);

@@ -1,5 +1,6 @@
 """What the kernels' sources have to keep to (CPU)."""
 import os
+import re
 
 import pytest
 
@@ -15,3 +16,14 @@ def test_early_launched_kernels_read_by_plain_loads(name):
         source = f.read()
     for load in ("__ldg", "ld.global.nc", "__restrict__"):
         assert load not in source
+
+
+def test_rounds_of_histograms_take_turns():
+    """A thread late in reading where a round's boundary lies must not meet what the next round's first threads store
+    there, as no barrier stands between the two: every access within the rounds is to the round's own slot."""
+    with open(os.path.join(_build.CSRC, "sample.cu")) as f:
+        source = f.read()
+    rounds = source[source.index("auto boundary = ["):source.index("// ---- draw in ascending order")]
+    shared = [w for name in ("cut", "above") for w in re.findall(r"\bs\." + name + r"\w*(?:\[\w+\])?", rounds)]
+    assert len(shared) >= 5 and all(w.endswith("[turn]") for w in shared), shared
+    assert "turn ^= 1" in rounds

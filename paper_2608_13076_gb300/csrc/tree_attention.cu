@@ -74,7 +74,8 @@ struct Params {
 __host__ __device__ constexpr int part_floats(int D) { return kRows * D + 2 * kRows; }
 
 constexpr int kBarKFull = 0, kBarKEmpty = 2, kBarVFull = 4, kBarVReady = 6, kBarVEmpty = 8, kBarSFull = 10, kBarPFull = 12,
-              kBarOFinal = 14, kBarOFree = 16, kBarQFull = 18, kBarQFree = 20, kBarPHalf = 21, kBarDrain = 23, kBarBad = 24, kNumBars = kBarBad + kBadRing;
+              kBarOFinal = 14, kBarOFree = 16, kBarQFull = 18, kBarQFree = 20, kBarPHalf = 21, kBarDrain = 23, kBarBad = 24, kBarStart = kBarBad + kBadRing,
+              kNumBars = kBarStart + 1;
 
 // A CTA's range of the cost space: of `num_ctas` ranges the first `longer` are one longer than `size`.
 struct Range {
@@ -405,6 +406,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       for (int i = 0; i < kBadRing; ++i) mbar_init(&bars[kBarBad + i], 1);
       mbar_init(&bars[kBarQFree], 1);
       mbar_init(&bars[kBarDrain], 1);
+      mbar_init(&bars[kBarStart], 1);
       fence_mbar_init();
     }
     __syncwarp();
@@ -507,8 +509,9 @@ __global__ void __launch_bounds__(kThreads, 1)
           row_b = slices == 2 ? uniform(paged_row(p, b, kvh, key0 + 64)) : 0;
         }
         uint8_t *tile = ring + st * kTile;
-        // (The first values wait until the first queries have come: scores need those and one tile of keys.)
-        if (is_v && it == 0) ok = wait_short(&bars[kBarQFull], 0, s_abort);
+        // (The first values wait until the first queries have come: scores need those and one tile of keys.  The barrier of
+        // the queries themselves may have gone on to the next ones before this warp looks at it; this one completes once.)
+        if (is_v && it == 0) ok = wait_short(&bars[kBarStart], 0, s_abort);
         ok = ok && wait_short(&empty[st], ((it / kStages) & 1) ^ 1, s_abort);
         if (!ok) break;
         if (leader) {
@@ -572,6 +575,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const bool dual = uniform(s_kd[b]) + 1 - uniform(g.group) * 2 * p.tile_nodes > p.tile_nodes;
       const int nsteps = dual ? 2 * n : n;
       ok = wait_short(&bars[kBarQFull], seg & 1, s_abort);
+      if (seg == 0 && lane == 0) mbar_arrive(&bars[kBarStart]);
       auto wait_k = [&](int j) {
         const uint32_t it = it0 + (dual ? j >> 1 : j);
         ok &= wait_short(&bars[kBarKFull + it % kStages], (it / kStages) & 1, s_abort);

@@ -341,3 +341,20 @@ def test_a_sequence_without_drafts_among_others(gpu_lib):
                             acc, nxt, path, new, max_k=0, status=st)
     assert acc.tolist() == [0, 0] and nxt.tolist() == [4, 9] and path.tolist() == [0, 0] and new.tolist() == [6, 1]
     assert int(st.item()) == 0
+
+
+@pytest.mark.parametrize("page", [0, 64])
+def test_ranges_that_begin_with_one_chunk(gpu_lib, page):
+    """Many short units: a CTA's range often begins with one last chunk of a unit and goes on with another's."""
+    rng = np.random.RandomState(7)
+    ctx, k = rng.randint(0, 700, 96).tolist(), rng.randint(0, 3, 96).tolist()
+    c = T.cache(ctx, k, 4, 128, page, 131, DEV)
+    q = T.queries(c, 2, 132)
+    mask = T.tree_mask(T.parents(k, "tree", 133), k, c["cu"].cpu())
+    ws = gpu_lib.tree_attn_workspace(c["B"], 8, 4, 128, c["cap"], c["max_k"])
+    out, lse, st = T.attention(c, q, mask, workspace=ws)
+    assert int(st.item()) == 0
+    T.check_attention(c, q, mask, out, lse)
+    for _ in range(50):
+        again, l2, st = T.attention(c, q, mask, workspace=ws)
+        assert int(st.item()) == 0 and torch.equal(out, again) and torch.equal(lse, l2)

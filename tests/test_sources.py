@@ -27,3 +27,14 @@ def test_rounds_of_histograms_take_turns():
     shared = [w for name in ("cut", "above") for w in re.findall(r"\bs\." + name + r"\w*(?:\[\w+\])?", rounds)]
     assert len(shared) >= 5 and all(w.endswith("[turn]") for w in shared), shared
     assert "turn ^= 1" in rounds
+
+
+def test_the_start_of_the_values_waits_for_a_barrier_that_completes_once():
+    """A wait by parity has to look before the barrier's next phase ends.  Nothing holds the queries' barrier back for the
+    warp that copies values, which is no user of them: it waits for one that is arrived at once."""
+    with open(os.path.join(_build.CSRC, "tree_attention.cu")) as f:
+        source = f.read()
+    waits = re.findall(r"if \(is_v && it == 0\) ok = wait_short\(&bars\[(\w+)\], 0, s_abort\);", source)
+    assert waits == ["kBarStart"]
+    assert re.findall(r"if \((.*)\) mbar_arrive\(&bars\[kBarStart\]\);", source) == ["seg == 0 && lane == 0"]
+    assert len(re.findall("kBarStart", source)) == 5  # its number twice, its initialisation, the wait, the arrival

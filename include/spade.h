@@ -658,7 +658,8 @@ spade_status spade_verify_rope_paged(const void *qkv, int64_t qkv_stride, const 
  *   tree_mask  int32 [R, mask_words], as above
  *   workspace  at least spade_tree_attn_workspace_size(...) bytes, 256-byte aligned,
  *              ZEROED ONCE (and again after a call that set SPADE_DEV_TIMEOUT);
- *              calls that share one must be ordered
+ *              calls of any sizes may share one that is large enough for each,
+ *              ordered
  * Everything else is as for spade_verify_attention and its paged form (pages of a
  * multiple of 64 slots).  The softmax weights are rounded to bf16 (2^-8 of
  * themselves) on their way into the product with the values, sums are fp32.
@@ -679,7 +680,8 @@ spade_status spade_verify_attention_tree_paged(
     void *workspace, size_t workspace_bytes, int32_t *status, spade_stream_t stream);
 
 /* Bytes of workspace that the two calls above need for these sizes on the current
- * device (cap: max_pages * page_size for the paged form; 0 on invalid sizes). */
+ * device (cap: max_pages * page_size for the paged form; 0 on invalid sizes).  They
+ * are the same for all sizes of a head dim. */
 size_t spade_tree_attn_workspace_size(int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t cap,
                                       int32_t max_k);
 

@@ -517,7 +517,8 @@ def spade_tree_attn_workspace_size(B, Hq, Hkv, D, cap, max_k):
 
 
 def tree_attn_workspace(B, Hq, Hkv, D, cap, max_k, device="cuda"):
-    """A zeroed workspace for spade_verify_attention_tree (zeroed once; calls keep its counters zeroed)."""
+    """A zeroed workspace for spade_verify_attention_tree (zeroed once; calls keep its counters zeroed).  Calls of other sizes
+    may use it too, one after the other, if it is large enough for them: its size depends on the head dim alone."""
     n = spade_tree_attn_workspace_size(B, Hq, Hkv, D, cap, max_k)
     if n == 0:
         raise SpadeError(-1, "spade_tree_attn_workspace_size returned 0: " + load().spade_last_error().decode())

@@ -57,14 +57,13 @@ struct Params {
   __nv_bfloat16 *out;
   float *lse;
   const int32_t *ctx_lens, *n_draft, *cu_q, *mask;
-  int32_t *counters;  // [units][2 tiles]{parts finished, parts written}, zero between calls
-  int32_t *groups;    // [num_ctas][2 segments][2 tiles]: the parts that a group has
+  int32_t *counters;  // [num_ctas][2 tiles]{parts finished, parts written} of the split unit that begins in a CTA's range
+  int32_t *groups;    // [num_ctas][2 segments][2 tiles]: the parts that a group has.  Zero between calls, as the counters are
   float *partials;    // [num_ctas][2 segments][2 tiles][part_floats(D)]
   int32_t *status;
   const int32_t *block_table;  // null: dense
   int B, Hq, Hkv, G, cap, max_k, R, words;
   int tile_nodes;     // nodes of a tile: 128 / G
-  int units_max;      // row groups of a KV head, by max_k
   int num_ctas;
   int page_size, max_pages, num_pages;
   float scale_log2;
@@ -906,7 +905,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       auto ml_at = [&](int i) {  // its m; kRows behind that, its l
         return reinterpret_cast<const float *>(part_at(i) - row) + kRows * D + row;
       };
-      int32_t *counter = p.counters + 4 * static_cast<int64_t>((g.b * p.Hkv + g.kvh) * p.units_max + g.group) + 2 * tile;
+      // (Of the units that begin in a CTA's range only the last goes on in another's.)
+      int32_t *counter = p.counters + 4 * c_first + 2 * tile;
       const bool many = nparts > kMany;
       bool last = !many;
       if (writes && nparts > 1 && !many) {
@@ -1055,7 +1055,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 }
 
 // The sizes that the kernel's 32-bit numbers and the schedule hold.
-static spade_status check_sizes(const char *name, int B, int Hq, int Hkv, int D, int cap, int max_k, int *units_max) {
+static spade_status check_sizes(const char *name, int B, int Hq, int Hkv, int D, int cap, int max_k) {
   if (B <= 0 || Hq <= 0 || Hkv <= 0 || cap <= 0 || max_k < 0) return fail(SPADE_ERR_INVALID_ARG, "%s: non-positive size", name);
   if (Hq % Hkv) return fail(SPADE_ERR_SHAPE, "%s: Hq (%d) must be a multiple of Hkv (%d)", name, Hq, Hkv);
   if (D != 64 && D != 128) return fail(SPADE_ERR_SHAPE, "%s: head dim %d not supported (64 or 128)", name, D);
@@ -1067,22 +1067,23 @@ static spade_status check_sizes(const char *name, int B, int Hq, int Hkv, int D,
   const int64_t groups = most / nodes2 + 1, units = static_cast<int64_t>(B) * Hkv * groups;
   // (The chunks of all units, with the virtual ones, too.)
   const int64_t chunks = (static_cast<int64_t>(cap) + kKeys - 1) / kKeys + kUnitCost;
-  if (cap > INT32_MAX - 2 * kKeys || 4 * units > INT32_MAX || units * chunks > INT32_MAX - 2 * kThreads)
+  if (cap > INT32_MAX - 2 * kKeys || units > INT32_MAX / 4 || units * chunks > INT32_MAX - 2 * kThreads)
     return fail(SPADE_ERR_CAPACITY, "%s: %d x %d KV heads, %d slots and max_k = %d leave 32-bit numbers", name, B, Hkv, cap, max_k);
-  *units_max = static_cast<int>(groups);
   return SPADE_OK;
 }
 
-// Counters of units, and of groups of parts.
-static size_t counter_bytes(int64_t units, int sms) {
-  return round_up(static_cast<size_t>(units) * 16, 256) + round_up(static_cast<size_t>(sms) * 16, 256);
+// The workspace: counters of split units, those of groups of parts, the parts.  Where the counters lie depends on the device
+// alone, so that calls of all sizes find them as the last call left them, whatever it was.
+static size_t counter_bytes(int sms) { return round_up(static_cast<size_t>(sms) * 16, 256); }
+static size_t workspace_bytes_of(int sms, int D) {
+  return 2 * counter_bytes(sms) + static_cast<size_t>(sms) * 4 * part_floats(D) * sizeof(float);
 }
 
 static spade_status attend(const char *name, Params p, const void *q, const void *k, const void *v, int D, int64_t cache_rows,
                            void *workspace, size_t workspace_bytes, cudaStream_t stream) {
   if (!q || !k || !v || !p.ctx_lens || !p.n_draft || !p.cu_q || !p.mask || !p.out || !p.status)
     return fail(SPADE_ERR_INVALID_ARG, "%s: null pointer argument", name);
-  spade_status st = check_sizes(name, p.B, p.Hq, p.Hkv, D, p.cap, p.max_k, &p.units_max);
+  spade_status st = check_sizes(name, p.B, p.Hq, p.Hkv, D, p.cap, p.max_k);
   if (st != SPADE_OK) return st;
   if (p.R <= 0 || p.R < p.B) return fail(SPADE_ERR_INVALID_ARG, "%s: R = %d < B = %d", name, p.R, p.B);
   if (p.words < p.max_k / 32 + 1)
@@ -1094,13 +1095,12 @@ static spade_status attend(const char *name, Params p, const void *q, const void
   int sms = 0;
   st = device_info(&sms, nullptr);
   if (st != SPADE_OK) return st;
-  const int64_t units = static_cast<int64_t>(p.B) * p.Hkv * p.units_max;
-  const size_t need = counter_bytes(units, sms) + static_cast<size_t>(sms) * 4 * part_floats(D) * sizeof(float);
+  const size_t need = workspace_bytes_of(sms, D);
   if (!workspace || workspace_bytes < need || !aligned(workspace, 256))
     return fail(SPADE_ERR_WORKSPACE, "%s: workspace needs %zu bytes, 256-byte aligned (got %zu)", name, need, workspace_bytes);
   p.counters = static_cast<int32_t *>(workspace);
-  p.groups = p.counters + counter_bytes(units, 0) / 4;
-  p.partials = reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + counter_bytes(units, sms));
+  p.groups = p.counters + counter_bytes(sms) / 4;
+  p.partials = reinterpret_cast<float *>(p.groups + counter_bytes(sms) / 4);
   p.G = p.Hq / p.Hkv;
   p.tile_nodes = kRows / p.G;
   p.scale_log2 = 1.4426950408889634f / sqrtf(static_cast<float>(D));
@@ -1135,11 +1135,10 @@ static spade_status attend(const char *name, Params p, const void *q, const void
 using namespace spade;
 
 extern "C" size_t spade_tree_attn_workspace_size(int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t cap, int32_t max_k) {
-  int units_max = 0, sms = 0;
-  if (attn_tree::check_sizes("spade_tree_attn_workspace_size", B, Hq, Hkv, D, cap, max_k, &units_max) != SPADE_OK) return 0;
+  int sms = 0;
+  if (attn_tree::check_sizes("spade_tree_attn_workspace_size", B, Hq, Hkv, D, cap, max_k) != SPADE_OK) return 0;
   if (device_info(&sms, nullptr) != SPADE_OK) return 0;
-  return attn_tree::counter_bytes(static_cast<int64_t>(B) * Hkv * units_max, sms) +
-         static_cast<size_t>(sms) * 4 * attn_tree::part_floats(D) * sizeof(float);
+  return attn_tree::workspace_bytes_of(sms, D);
 }
 
 extern "C" spade_status spade_verify_attention_tree(const void *q, const void *k_cache, const void *v_cache,

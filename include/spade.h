@@ -157,8 +157,9 @@ size_t spade_qkv_workspace_size(int32_t R, int32_t Hq, int32_t Hkv, int32_t D);
  *              pass 31 bits are refused with SPADE_ERR_CAPACITY)
  *   workspace  device scratch of at least spade_attn_workspace_size(...) bytes,
  *              256-byte aligned, ZEROED ONCE by the caller after allocation;
- *              every call that completes leaves it zeroed again.  Calls that
- *              share a workspace must be ordered (same stream or events).
+ *              every call that completes leaves it ready for the next, of any
+ *              sizes it is large enough for.  Calls that share a workspace must
+ *              be ordered (same stream or events).
  *   status     device int32, SPADE_DEV_* bits OR-ed in
  * Slots beyond ctx_b + k_b are never read into the result, whatever they hold.
  */

@@ -29,7 +29,7 @@ struct Params {
   const int32_t *ctx_lens;
   const int32_t *n_draft;
   const int32_t *cu_q;
-  int32_t *counters;  // [units], zero between calls
+  int32_t *counters;  // [num_ctas]: of the split unit whose slices begin in a CTA's range; zero between calls
   float *partials;    // [(num_ctas + units) slots][kRowBlock * D + 2 * kRowBlock]
   int32_t *status;
   int B, Hq, Hkv, G, cap, max_k, R, RB, num_ctas;
@@ -57,6 +57,10 @@ __device__ __forceinline__ int paged_row(const Params &p, int b, int kvh, int ke
 }
 
 constexpr int round_up_c(int x, int a) { return (x + a - 1) / a * a; }
+
+// The counters' bytes, in front of the parts.  Both lie where they lie whatever a call's sizes are, so that calls of all
+// sizes find the counters as the last call left them.
+inline size_t counter_bytes(int sms) { return round_up(static_cast<size_t>(sms) * 4, 256); }
 
 // Refuses sizes that the kernels' 32-bit numbers do not hold: a KV head has G (max_k + 1) rows, a
 // mask multiplies G by positions up to two slices past the last, there are B * Hkv units per row

@@ -56,8 +56,7 @@ extern "C" spade_status spade_verify_attention_kv4(
   p.n_draft = n_draft;
   p.cu_q = cu_q;
   p.counters = static_cast<int32_t *>(workspace);
-  p.partials = reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) +
-                                         round_up(static_cast<size_t>(units) * 4, 256));
+  p.partials = reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + attn::counter_bytes(sms));
   p.status = status;
   p.B = B; p.Hq = Hq; p.Hkv = Hkv; p.G = G; p.cap = cap; p.max_k = max_k; p.R = R; p.RB = RB;
   p.scale_log2 = 1.4426950408889634f / sqrtf(static_cast<float>(D));

@@ -29,8 +29,7 @@ extern "C" size_t spade_attn_workspace_size(int32_t B, int32_t Hq, int32_t Hkv, 
   if (device_info(&sms, nullptr) != SPADE_OK) return 0;
   const int RB = attn::row_blocks(Hq / Hkv, max_k);
   const size_t units = static_cast<size_t>(B) * Hkv * RB;
-  const size_t counters = round_up(units * 4, 256);
-  return counters + (units + sms) * attn::slot_floats(D) * sizeof(float);
+  return attn::counter_bytes(sms) + (units + sms) * attn::slot_floats(D) * sizeof(float);
 }
 
 namespace spade {
@@ -83,8 +82,7 @@ static spade_status verify_attention_impl(
   p.n_draft = n_draft;
   p.cu_q = cu_q;
   p.counters = static_cast<int32_t *>(workspace);
-  p.partials = reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) +
-                                         round_up(static_cast<size_t>(units) * 4, 256));
+  p.partials = reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + attn::counter_bytes(sms));
   p.status = status;
   p.B = B; p.Hq = Hq; p.Hkv = Hkv; p.G = G; p.cap = cap; p.max_k = max_k; p.R = R; p.RB = RB;
   p.scale_log2 = 1.4426950408889634f / sqrtf(static_cast<float>(D));
@@ -195,8 +193,8 @@ extern "C" spade_status spade_verify_attention_noalloc(
   if (D != 64 && D != 128) return fail(SPADE_ERR_SHAPE, "head dim %d not supported (64 or 128)", D);
   spade_status st = attn::check_rows("spade_verify_attention_noalloc", B, Hkv, Hq / Hkv, max_k, cap);
   if (st != SPADE_OK) return st;
-  int dev = 0;
-  st = device_info(nullptr, &dev);
+  int dev = 0, sms = 0;
+  st = device_info(&sms, &dev);
   if (st != SPADE_OK) return st;
   if (dev >= kMaxDevices) return fail(SPADE_ERR_UNSUPPORTED_DEVICE, "device %d", dev);
   const size_t need = spade_attn_workspace_size(B, Hq, Hkv, D, cap, max_k);
@@ -211,9 +209,7 @@ extern "C" spade_status spade_verify_attention_noalloc(
   if (st != SPADE_OK) return st;
   // The merge counters must start at zero; the array keeps whatever the last
   // call (possibly an interrupted one) left there.
-  const size_t units = static_cast<size_t>(B) * Hkv * attn::row_blocks(Hq / Hkv, max_k);
-  const cudaError_t e = cudaMemsetAsync(scratch, 0, round_up(units * 4, 256),
-                                        reinterpret_cast<cudaStream_t>(stream));
+  const cudaError_t e = cudaMemsetAsync(scratch, 0, attn::counter_bytes(sms), reinterpret_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return cuda_fail(e, "cudaMemsetAsync(attention scratch counters)");
   return spade_verify_attention(q, k_cache, v_cache, ctx_lens, n_draft, cu_q, out, lse, B, Hq, Hkv,
                                 D, cap, max_k, R, scratch, kScratchBytes, status, stream);

@@ -620,13 +620,14 @@ __global__ void __launch_bounds__(kThreads, 1)
           __stcg(part + kRowBlock * kD + kRowBlock + c0 + lane, l_own);
         }
         named_bar(1, kSoftThreads);
-        if (stid == 0) *s_last = arrive_part(&p.counters[unit], nparts);
+        // (Of the units whose slices begin in a CTA's range only the last goes on in another's.)
+        if (stid == 0) *s_last = arrive_part(&p.counters[c_first], nparts);
         named_bar(1, kSoftThreads);
         if (*s_last) {
           // This CTA finished the unit last: merge every partial by log-sum-exp.
           static_assert(kSoftWarps == kMergeWarps, "the softmax warps merge");
           merge_partials<kD>(p, c_first + unit, nparts, nrow, g.rb, g.kvh, q_row0, s_wred, stid, warp - 2, lane);
-          if (stid == 0) p.counters[unit] = 0;  // every part has arrived: reset for the next call
+          if (stid == 0) p.counters[c_first] = 0;  // every part has arrived: reset for the next call
         }
       }
       ++seg;

@@ -701,8 +701,8 @@ size_t spade_tree_attn_workspace_size(int32_t B, int32_t Hq, int32_t Hkv, int32_
  *   included), as in spade_verify_accept_sampling;
  *   of those, tokens with p(x) >= min_p[r] times the largest p;
  * as the smallest x whose cumulative mass in ascending order exceeds uniforms[r]
- * times the whole.  The decisions are those of 64-bit arithmetic (weights to 2^-39,
- * exact sums), not of fp32 sums.
+ * times the whole.  The decisions are those of 64-bit arithmetic (weights to 2^-39 of
+ * themselves or 2^-60 of the largest, exact sums), not of fp32 sums.
  *   logits       [R, V] of `dtype` (SPADE_F32, SPADE_BF16, SPADE_F16), rows
  *                row_stride elements apart; -infinity excludes a token
  *   uniforms     float32 [R] in [0, 1)

@@ -3,8 +3,9 @@
 //
 // The tokens are those of the definition in 64 bits (but for uniforms within about 2^-36 of an
 // edge), not of fp32 sums: a weight 2^((l - m) log2(e) / T) is computed to 2^-39 of itself and
-// summed as a whole number, in units of 2^-shift of the largest, so sums are exact, whatever
-// their order.
+// summed as a whole number, in units of 2^-60 of the largest, so sums are exact, whatever their order, and a
+// tail of a million tokens below the unit is off by 2^-40 at most.  (Sums are 128 bits wide; 64 leave a million
+// tokens a unit of 2^-42 and an error of 2^-22.)  Where few tokens are summed the unit is 2^-50.
 //
 // A cluster of CTAs takes a row: each copies its part once into shared memory, and what follows (the
 // largest logit, counts, sums) meets through distributed shared memory.  The kept set is always
@@ -65,7 +66,7 @@ struct Params {
   float *probs, *chosen;
   int64_t stride;  // of the logits' rows, in elements
   int V, slice;    // slice: 16-byte vectors of a CTA
-  int shift;       // unit of the sums: 2^-shift of the largest weight
+  int shift;       // unit of the rough draw's sums: 2^-shift of the largest weight
 };
 
 // 2^(j / 256) in units of 2^-40, by the exponential series at compile time.
@@ -90,8 +91,14 @@ __device__ constexpr Powers kPowers = make_powers();
 struct Row {
   float m;       // largest logit
   float ch, cl;  // log2(e) / T, high and low part
-  int shift;
 };
+
+// Sums of weights in units of 2^-kMassShift of the largest: 2^21 weights of up to 2^60, and a product with a number of 24
+// bits, stay below 2^106.  A vector's sum is below 2^64.
+using Mass = unsigned __int128;
+constexpr int kMassShift = 60;
+// The unit of a list of up to kList tokens: its sums stay below 2^62, and what is below it makes 2^-39.
+constexpr int kListShift = 50;
 
 // Weight of a logit relative to the largest, as 2^40 .. 2^41 times 2^(-40 - e) (e < 0: it is 0).
 // With x = (l - m) log2(e) / T = n / 256 + r, |r| <= 1/512, the weight is 2^(n/256) (1 + y),
@@ -134,12 +141,13 @@ SPADE_DEVICE float weight_about(const Row &w, float l) {
   const float q = ex2(ph);
   return s == 0.f ? 1.f : ph > -120.f ? fmaf(q * pl, 0.693147181f, q) : 0.f;
 }
-// The weight in units of 2^-shift; at least one unit if it is not 0.
+// The weight in units of 2^-kMassShift, or of a list; at least one unit if it is not 0.
+template <int kShift = kMassShift>
 SPADE_DEVICE uint64_t weight(const Row &w, const uint64_t *powers, float l) {
   int e;
   const uint64_t v = weight40(w, powers, l, &e);
   if (e < 0) return 0;
-  const uint64_t u = e > 63 ? 0 : (v << (w.shift - 40)) >> e;
+  const uint64_t u = e > 63 ? 0 : v << (kShift - 40) >> e;
   return u ? u : 1;
 }
 
@@ -218,20 +226,36 @@ SPADE_DEVICE V warp_reduce(V v, F f) {
   return v;
 }
 SPADE_DEVICE uint64_t add64(uint64_t a, uint64_t b) { return a + b; }
-SPADE_DEVICE uint64_t warp_scan(uint64_t v, int lane) {  // inclusive
+SPADE_DEVICE uint64_t low_of(Mass v) { return static_cast<uint64_t>(v); }
+SPADE_DEVICE uint64_t high_of(Mass v) { return static_cast<uint64_t>(v >> 64); }
+SPADE_DEVICE Mass mass_of(uint64_t low, uint64_t high) { return static_cast<Mass>(high) << 64 | low; }
+SPADE_DEVICE uint64_t shuffled_up(uint64_t v, int o) { return __shfl_up_sync(0xffffffffu, v, o); }
+SPADE_DEVICE Mass shuffled_up(Mass v, int o) { return mass_of(shuffled_up(low_of(v), o), shuffled_up(high_of(v), o)); }
+SPADE_DEVICE uint64_t last_lane(uint64_t v) { return __shfl_sync(0xffffffffu, v, 31); }
+SPADE_DEVICE Mass last_lane(Mass v) { return mass_of(last_lane(low_of(v)), last_lane(high_of(v))); }
+template <class V>
+SPADE_DEVICE V warp_scan(V v, int lane) {  // inclusive
 #pragma unroll
   for (int o = 1; o < 32; o *= 2) {
-    const uint64_t x = __shfl_up_sync(0xffffffffu, v, o);
+    const V x = shuffled_up(v, o);
     if (lane >= o) v += x;
   }
+  return v;
+}
+SPADE_DEVICE uint64_t warp_add(uint64_t v) { return warp_reduce(v, add64); }
+SPADE_DEVICE Mass warp_add(Mass v) {
+#pragma unroll
+  for (int o = 16; o; o /= 2)
+    v += mass_of(__shfl_xor_sync(0xffffffffu, low_of(v), o), __shfl_xor_sync(0xffffffffu, high_of(v), o));
   return v;
 }
 
 struct Shared {
   uint64_t powers[256];
   uint64_t list[kLocal];     // the part's listed tokens: order (descending) and index; read by the leader
-  uint32_t hist[kBins], high[kBins];  // counts, or masses' low and high halves
+  uint32_t hist[kBins], mid[kBins], high[kBins];  // counts, or the three words of masses
   uint64_t warp[kWarps];     // results of the warps
+  Mass wide[kWarps];
   uint64_t sums[2][kWarps];
   float masses[2][kWarps];
   uint64_t meet[2][3][kMaxCluster];  // results of the cluster's CTAs, by turns
@@ -240,7 +264,7 @@ struct Shared {
   uint32_t count, settled;
   int cut;
   int cuts[2];               // a round of histograms' boundary bin, and what is above it: by turns, as a thread late in
-  uint64_t above[2];         // reading one round's must not find the next round's
+  Mass above[2];             // reading one round's must not find the next round's
   float ch, cl, tau;         // log2(e) / T, high and low part
 };
 
@@ -293,16 +317,37 @@ struct Team {
     for (int i = 1; i < size; ++i) r = f(r, all[0][i]);
     return r;
   }
+  // Sums of masses over the CTA's threads and over the cluster, on every thread.
+  SPADE_DEVICE Mass block_sum(Mass v) {
+    v = warp_add(v);
+    if (lane == 0) s->wide[warp] = v;
+    __syncthreads();
+    Mass r = s->wide[0];
+    for (int i = 1; i < kWarps; ++i) r += s->wide[i];
+    __syncthreads();
+    return r;
+  }
+  SPADE_DEVICE Mass cluster_sum(Mass v) {
+    v = block_sum(v);
+    const uint64_t(*all)[kMaxCluster] = exchange(2, low_of(v), high_of(v), 0);
+    Mass r = 0;
+    for (int i = 0; i < size; ++i) r += mass_of(all[0][i], all[1][i]);
+    return r;
+  }
 };
 
-// f * total for f in [0, 1], rounded down (whole: up).
-SPADE_DEVICE uint64_t part_of(float f, uint64_t total, bool up) {
-  if (f >= 1.f) return total;
+// f = digits 2^-q, q >= 24, of f in [0, 1).
+SPADE_DEVICE uint32_t digits_of(float f, int *q) {
   const uint32_t bits = __float_as_uint(f);
   const int exponent = static_cast<int>(bits >> 23);
-  const uint64_t digits = (bits & 0x7fffffu) | (exponent ? 0x800000u : 0u);
-  const int q = 150 - (exponent ? exponent : 1);  // f = digits 2^-q, q >= 24
-  const uint64_t hi = __umul64hi(total, digits), lo = total * digits;
+  *q = 150 - (exponent ? exponent : 1);
+  return (bits & 0x7fffffu) | (exponent ? 0x800000u : 0u);
+}
+// f * total for f in [0, 1], rounded down (up: up).
+SPADE_DEVICE uint64_t part_of(float f, uint64_t total, bool up) {
+  if (f >= 1.f) return total;
+  int q;
+  const uint64_t digits = digits_of(f, &q), hi = __umul64hi(total, digits), lo = total * digits;
   uint64_t t = 0;
   bool rest;
   if (q < 64) {
@@ -314,9 +359,19 @@ SPADE_DEVICE uint64_t part_of(float f, uint64_t total, bool up) {
   }
   return t + (up && rest);
 }
+SPADE_DEVICE Mass part_of(float f, Mass total, bool up) {
+  if (f >= 1.f) return total;
+  int q;
+  const Mass t = total * digits_of(f, &q), whole = q < 128 ? t >> q : 0;
+  return whole + (up && (q < 128 ? whole << q : 0) != t);
+}
+// x 2^kBits of a list, where all that matters of a bound past its sums is that it is.
+template <int kBits>
+SPADE_DEVICE uint64_t widened(uint64_t x) { return x >> (64 - kBits) ? ~0ull : x << kBits; }
 // Cumulative mass > u Z is cumulative mass > this.
-SPADE_DEVICE uint64_t target_of(float u, uint64_t total) {
-  const uint64_t t = part_of(u, total, false);
+template <class V>
+SPADE_DEVICE V target_of(float u, V total) {
+  const V t = part_of(u, total, false);
   return t < total ? t : total - 1;
 }
 SPADE_DEVICE float unit_of(uint64_t total, int shift) { return __fdiv_rn(static_cast<float>(uint64_t(1) << shift), static_cast<float>(total)); }
@@ -325,6 +380,12 @@ SPADE_DEVICE float share(const Row &w, const uint64_t *powers, float l, float un
   int e;
   const uint64_t v = weight40(w, powers, l, &e);
   return e < 0 ? 0.f : ldexpf(static_cast<float>(v) * unit, -40 - e);
+}
+// The same for one token, with a rounding less.
+SPADE_DEVICE float share_of(const Row &w, const uint64_t *powers, float l, uint64_t total, int shift) {
+  int e;
+  const uint64_t v = weight40(w, powers, l, &e);
+  return e < 0 ? 0.f : ldexpf(__fdiv_rn(static_cast<float>(v), static_cast<float>(total)), shift - 40 - e);
 }
 
 // The sum over a warp's lanes on every lane, by the 32-bit reductions of 20, 20 and 24 bits.
@@ -397,7 +458,7 @@ SPADE_DEVICE void decide(const Params &p, Shared &s, Team &team, const Row &w, u
     const uint64_t key = i < n ? keys[i] : ~0ull;
     order[e] = static_cast<uint32_t>(key >> 32);
     index[e] = static_cast<uint32_t>(key);
-    own[e] = i < n ? weight(w, powers, number_of(~order[e])) : 0;
+    own[e] = i < n ? weight<kListShift>(w, powers, number_of(~order[e])) : 0;
   }
   // Orders of listed tokens, without the bits that the type's numbers share.
   const uint32_t least = ~order_of(w.m) >> T::kSpare, most_order = ~order_of(bound) >> T::kSpare;
@@ -441,10 +502,12 @@ SPADE_DEVICE void decide(const Params &p, Shared &s, Team &team, const Row &w, u
     uint64_t all = total_of();
     uint64_t goal = part_of(top_p, all, true), most = goal;
     if (!has_k) {
-      // The row's mass, known to 2^-16 of what is not listed: where that does not settle every token, exactly.
-      const uint64_t rest = w.shift >= 40 ? out_mass << (w.shift - 40) : out_mass >> (40 - w.shift);
-      most = part_of(top_p, all + rest + (rest >> 16) + p.V + (kThreads * kMaxCluster << 4), true);
-      goal = part_of(top_p, all + (rest - (rest >> 16)), true);
+      // The row's mass, in units of 2^-40 and known to 2^-16 of what is not listed: where that does not settle every
+      // token, exactly.
+      constexpr int kBits = kListShift - 40;
+      const uint64_t slack = out_mass >> 16;
+      most = widened<kBits>(part_of(top_p, (all >> kBits) + 1 + out_mass + slack + (p.V >> kBits) + 1 + kThreads * kMaxCluster, true));
+      goal = widened<kBits>(part_of(top_p, (all >> kBits) + out_mass - slack, false));
     }
     for (int exact = 0; exact < 2; ++exact) {
       bool open = false;
@@ -465,14 +528,17 @@ SPADE_DEVICE void decide(const Params &p, Shared &s, Team &team, const Row &w, u
         else if (larger >= goal) own[0] = 0;
         break;
       }
-      uint64_t v = 0;
+      Mass v = 0;
       for (int i = tid; i < p.V; i += kThreads) {
         uint4 x = make_uint4(0, 0, 0, 0);
         if constexpr (T::kSize == 4) x.x = reinterpret_cast<const uint32_t *>(row)[i];
         else x.x = reinterpret_cast<const uint16_t *>(row)[i];
         v += weight(w, powers, T::number(x, 0));
       }
-      goal = most = part_of(top_p, team.block(v, add64), true);
+      // (In the list's units, rounded up: whole numbers reach it where they reach that.)
+      constexpr int kBits = kMassShift - kListShift;
+      const Mass units = (part_of(top_p, team.block_sum(v), true) + ((1 << kBits) - 1)) >> kBits;
+      goal = most = high_of(units) ? ~0ull : low_of(units);
     }
   }
   if (has_m) {
@@ -482,7 +548,7 @@ SPADE_DEVICE void decide(const Params &p, Shared &s, Team &team, const Row &w, u
       if (order[e] > last) own[e] = 0;
   }
   const uint64_t total = total_of();
-  const float unit = unit_of(total, p.shift);
+  const float unit = unit_of(total, kListShift);
   const uint64_t target = target_of(u, total);
   if (probs) {
 #pragma unroll
@@ -507,7 +573,7 @@ SPADE_DEVICE void decide(const Params &p, Shared &s, Team &team, const Row &w, u
   for (int e = 0; e < kPer; ++e)
     if (tid + e * kThreads < n && index[e] == drawn) {
       p.tokens[r] = static_cast<int32_t>(drawn);
-      if (p.chosen) p.chosen[r] = __fdiv_rn(static_cast<float>(own[e]), static_cast<float>(total));
+      if (p.chosen) p.chosen[r] = share_of(w, powers, number_of(~order[e]), total, kListShift);
     }
 }
 
@@ -621,7 +687,6 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
   });
   Row w;
   w.m = number_of(static_cast<uint32_t>(ends >> 32));
-  w.shift = p.shift;
   float *probs = p.probs ? p.probs + static_cast<int64_t>(r) * p.V : nullptr;
   auto number = [&](int x) {  // token x of this part
     const int i = x - first;
@@ -696,7 +761,7 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
 #pragma unroll
           for (int c = 0; c < kMaxCluster; ++c) n += part[c];
         }
-        const uint64_t counted = warp_scan(n, lane);
+        const uint64_t counted = warp_scan(static_cast<uint64_t>(n), lane);
         if (lane == 31) s.warp[warp] = counted;
         __syncthreads();
         uint64_t count = counted;
@@ -812,15 +877,15 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
     // ---- many tokens: rounds of histograms ----
     // The largest `g` (an order without the spare bits) such that tokens from it on reach `goal`, in counts or masses;
     // tokens are those from `lo` on, which reach it unless there are too few (then lo).
-    auto boundary = [&](uint32_t lo, uint64_t goal, bool masses) {
+    auto boundary = [&](uint32_t lo, Mass goal, bool masses) {
       uint32_t hi = (order_of(w.m) >> T::kSpare) + 1;
-      uint64_t above = 0;  // of tokens from hi on
+      Mass above = 0;  // of tokens from hi on
       // First round: bins of equal width, to 24 T below the largest logit (or as far as the threads' largest reach).
       const float width = fmaxf(fminf(24.f * temp, FLT_MAX), w.m - number_of(~static_cast<uint32_t>(ends))) * (1.f / kBins);
       const float scale = __fdiv_rn(1.f, width);
       bool by_value = scale > 0.f && scale <= FLT_MAX;
       for (int turn = 0; hi - lo > 1; turn ^= 1) {
-        if (tid < kBins) s.hist[tid] = s.high[tid] = 0;
+        if (tid < kBins) s.hist[tid] = s.mid[tid] = s.high[tid] = 0;
         if (tid == 0) s.cuts[turn] = kBins;
         __syncthreads();
         int shift = 0;
@@ -843,25 +908,32 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
               b = (hi - 1 - g) >> shift;
             }
             if (masses) {
+              // (The third word takes what a bin of sixteen largest weights carries over.)
               const uint64_t q = weight(w, powers, l);
               const uint32_t low = static_cast<uint32_t>(q), old = atomicAdd(&s.hist[b], low);
-              const uint32_t carry = static_cast<uint32_t>(q >> 32) + (old + low < old);
-              if (carry) atomicAdd(&s.high[b], carry);
+              const uint32_t mid = static_cast<uint32_t>(q >> 32) + (old + low < old);
+              if (mid) {
+                const uint32_t was = atomicAdd(&s.mid[b], mid);
+                if (was + mid < was) atomicAdd(&s.high[b], 1u);
+              }
             } else {
               atomicAdd(&s.hist[b], 1u);
             }
           }
         }
         cluster_sync();
-        uint64_t n = 0;
+        Mass n = 0;
         if (tid < kBins)
-          for (int c = 0; c < team.size; ++c)
-            n += static_cast<uint64_t>(ld_cluster32(cluster_map(&s.high[tid], c))) << 32 | ld_cluster32(cluster_map(&s.hist[tid], c));
-        const uint64_t incl = warp_scan(n, lane);
-        if (lane == 31) s.warp[warp] = incl;
+          for (int c = 0; c < team.size; ++c) {
+            const uint32_t low = ld_cluster32(cluster_map(&s.hist[tid], c));
+            const uint64_t mid = ld_cluster32(cluster_map(&s.mid[tid], c));
+            n += mass_of(mid << 32 | low, ld_cluster32(cluster_map(&s.high[tid], c)));
+          }
+        const Mass incl = warp_scan(n, lane);
+        if (lane == 31) s.wide[warp] = incl;
         __syncthreads();
-        uint64_t upto = above + incl;
-        for (int i = 0; i < warp; ++i) upto += s.warp[i];
+        Mass upto = above + incl;
+        for (int i = 0; i < warp; ++i) upto += s.wide[i];
         if (tid < kBins && upto >= goal && upto - n < goal) {
           s.cuts[turn] = tid;
           s.above[turn] = upto - n;
@@ -878,9 +950,9 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
       return lo;
     };
     uint32_t edge = order_of(-FLT_MAX) >> T::kSpare;
-    if (has_k) edge = boundary(edge, static_cast<uint64_t>(k), false);
+    if (has_k) edge = boundary(edge, static_cast<Mass>(k), false);
     if (has_p) {
-      uint64_t whole = 0;
+      Mass whole = 0;
       for (int i = tid; i < n_vec; i += kThreads) {
         const uint4 x = s_vec[i];
 #pragma unroll
@@ -889,7 +961,7 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
           if (order_of(l) >> T::kSpare >= edge) whole += weight(w, powers, l);
         }
       }
-      whole = team.cluster(whole, add64);
+      whole = team.cluster_sum(whole);
       edge = boundary(edge, part_of(top_p, whole, true), true);
     }
     tau = fmaxf(tau, number_of(edge << T::kSpare));
@@ -898,20 +970,22 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
   // ---- draw in ascending order: sums of warps' stretches, of CTAs, then the stretch again ----
   const int per = (p.slice + kWarps - 1) / kWarps;
   const int w0 = min(warp * per, n_vec), w1 = min(w0 + per, n_vec);
-  uint64_t total = 0;
-  // Weights to 2^-20 first (sums of eight 2^-21): they settle the token where the target is further than their errors
-  // from its ends.  (With probabilities asked for, exact ones at once.)
-#pragma unroll 1
-  for (int exact = probs ? 1 : 0; exact < 2; ++exact) {
+  uint64_t total = 0;  // in units of 2^-40 where it is exact
+  // With sums of type M: exact ones, or 64 bits of weights known to 2^-20.  False: those do not settle the token.
+  auto draw = [&](auto sums) -> bool {
+    using M = decltype(sums);
+    constexpr bool exact = sizeof(M) > 8;
     const float units = static_cast<float>(uint64_t(1) << p.shift);
-    auto token_mass = [&](float l) {
-      return !(l >= tau) ? 0 : exact ? weight(w, powers, l) : __float2ull_rn(weight_about<T::kSize == 4>(w, l) * units);
+    auto token_mass = [&](float l) -> uint64_t {
+      if (!(l >= tau)) return 0;
+      if constexpr (exact) return weight(w, powers, l);
+      else return __float2ull_rn(weight_about<T::kSize == 4>(w, l) * units);
     };
     auto lane_mass = [&](int i) {  // of vector i's kept tokens
       uint64_t m = 0;
       if (i < w1) {
         const uint4 x = s_vec[i];
-        if (exact) {
+        if constexpr (exact) {
 #pragma unroll
           for (int e = 0; e < E; ++e) m += token_mass(T::number(x, e));
         } else {
@@ -927,40 +1001,45 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
       }
       return m;
     };
-    uint64_t mine = 0;
+    M mine = 0;
     for (int i = w0 + lane; i < w1; i += 32) mine += lane_mass(i);
-    mine = warp_reduce(mine, add64);
-    if (lane == 0) s.warp[warp] = mine;
+    mine = warp_add(mine);
+    if (lane == 0) s.wide[warp] = mine;
     if (tid == 0) s.settled = 0;
     __syncthreads();
-    uint64_t before = 0, part = 0;
+    M before = 0, part = 0;
     for (int i = 0; i < kWarps; ++i) {
-      if (i < warp) before += s.warp[i];
-      part += s.warp[i];
+      const M m = static_cast<M>(s.wide[i]);
+      if (i < warp) before += m;
+      part += m;
     }
-    const uint64_t *parts = team.exchange(1, part, 0, 0)[0];
-    total = 0;
+    const uint64_t(*parts)[kMaxCluster] = team.exchange(exact ? 2 : 1, low_of(part), exact ? high_of(part) : 0, 0);
+    M all = 0;
     for (int c = 0; c < team.size; ++c) {
-      if (c < team.rank) before += parts[c];
-      total += parts[c];
+      const M m = exact ? static_cast<M>(mass_of(parts[0][c], parts[1][c])) : static_cast<M>(parts[0][c]);
+      if (c < team.rank) before += m;
+      all += m;
     }
-    const uint64_t target = target_of(u, total), margin = exact ? 0 : 2 * ((total >> 20) + p.V);
+    total = exact ? low_of(all >> (kMassShift - 40)) : low_of(all);
+    // A token's end and the target differ by the weights before it times 1 - u less those behind times u: that is off by
+    // 2 u (1 - u) <= 1/2 of the weights' errors, 2^-20 and little more of the whole (roundings to units: one a token).
+    const M target = target_of(u, all), margin = exact ? 0 : static_cast<M>((low_of(all) >> 20) + p.V);
     if (target >= before && target < before + mine) {
       for (int i0 = w0; i0 < w1; i0 += 32) {
-        const uint64_t m = lane_mass(i0 + lane), upto = before + warp_scan(m, lane);
+        const M m = lane_mass(i0 + lane), upto = before + warp_scan(m, lane);
         const unsigned hit = __ballot_sync(0xffffffffu, upto > target);
         if (hit) {
           if (lane == __ffs(hit) - 1) {
-            uint64_t at = upto - m;
+            M at = upto - m;
             for (int e = 0; e < E; ++e) {
               const int x = first + (i0 + lane) * E + e;
               if (x < lo_x || x >= hi_x) continue;
-              const uint64_t q = token_mass(number(x));
+              const M q = token_mass(number(x));
               if (at + q > target) {
                 if (exact || (target >= at + margin && at + q >= target + margin)) {
                   s.settled = 1;
                   p.tokens[r] = x;
-                  if (p.chosen) p.chosen[r] = __fdiv_rn(static_cast<float>(weight(w, powers, number(x))), static_cast<float>(total));
+                  if (p.chosen) p.chosen[r] = share_of(w, powers, number(x), total, exact ? 40 : p.shift);
                 }
                 break;
               }
@@ -969,18 +1048,25 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
           }
           break;
         }
-        before = __shfl_sync(0xffffffffu, upto, 31);
+        before = last_lane(upto);
       }
     }
-    if (exact) break;
-    __syncthreads();
-    const uint64_t *done = team.exchange(1, s.settled, 0, 0)[0];
-    uint64_t settled = 0;
-    for (int c = 0; c < team.size; ++c) settled += done[c];
-    if (settled) return;
-  }
+    if constexpr (exact) {
+      return true;
+    } else {
+      __syncthreads();
+      const uint64_t *done = team.exchange(1, s.settled, 0, 0)[0];
+      uint64_t settled = 0;
+      for (int c = 0; c < team.size; ++c) settled += done[c];
+      return settled != 0;
+    }
+  };
+  // Weights to 2^-20 first (sums of eight 2^-21): they settle the token where the target is further than their errors
+  // from its ends.  (With probabilities asked for, exact ones at once.)
+  if (!probs && draw(uint64_t())) return;
+  draw(Mass());
   if (probs) {
-    const float unit = unit_of(total, p.shift);
+    const float unit = unit_of(total, 40);
     for (int x = lo_x + tid; x < hi_x; x += kThreads) {
       const float l = number(x);
       probs[x] = l >= tau ? share(w, powers, l, unit) : 0.f;
@@ -1045,7 +1131,7 @@ extern "C" spade_status spade_sample(const void *logits, int32_t dtype, int64_t 
   sample::plan(V, size, R, sms, &ctas, &p.slice);
   p.logits = logits; p.stride = row_stride; p.uniforms = uniforms; p.temperature = temperature; p.top_k = top_k;
   p.top_p = top_p; p.min_p = min_p; p.tokens = tokens; p.probs = probs; p.chosen = chosen; p.status = status; p.V = V;
-  // The sum of V weights of up to 2^shift stays below 2^62.
+  // (The rough draw's sum of V weights of up to 2^shift stays below 2^62.)
   int bits = 0;
   while ((int64_t(1) << bits) < V) ++bits;
   p.shift = 62 - bits < 44 ? 62 - bits : 44;

@@ -88,10 +88,14 @@ constexpr Powers make_powers() {
 }
 __device__ constexpr Powers kPowers = make_powers();
 
+// Where T is 2^64 and more, logits and T are 2^64 times smaller here: their differences stay finite, log2(e) / T stays
+// a normal number, and what a logit loses below 2^-126 is nothing beside T.
 struct Row {
-  float m;       // largest logit
-  float ch, cl;  // log2(e) / T, high and low part
+  float m;       // largest logit, times scale
+  float scale;   // 1 or 2^-64
+  float ch, cl;  // log2(e) / (T scale), high and low part
 };
+constexpr float kHuge = 18446744073709551616.f;  // 2^64
 
 // Sums of weights in units of 2^-kMassShift of the largest: 2^21 weights of up to 2^60, and a product with a number of 24
 // bits, stay below 2^106.  A vector's sum is below 2^64.
@@ -104,11 +108,11 @@ constexpr int kListShift = 50;
 // With x = (l - m) log2(e) / T = n / 256 + r, |r| <= 1/512, the weight is 2^(n/256) (1 + y),
 // y = e^(r ln 2) - 1 by four terms of its series, r and y held as pairs of fp32 numbers.
 SPADE_DEVICE uint64_t weight40(const Row &w, const uint64_t *powers, float l, int *e) {
-  const float s = l - w.m;
+  const float s = fmaf(l, w.scale, -w.m);
   *e = 0;
   if (s == 0.f) return uint64_t(1) << 40;
-  const float back = s - l;
-  const float rest = (l - (s - back)) + (-w.m - back);  // l - m = s + rest
+  const float x = l * w.scale, back = s - x;
+  const float rest = (x - (s - back)) + (-w.m - back);  // x - m = s + rest
   const float ph = s * w.ch;
   if (!(ph > -1075.f)) {  // less than the smallest number of 64 bits: 0
     *e = -1;
@@ -131,12 +135,12 @@ SPADE_DEVICE uint64_t weight40(const Row &w, const uint64_t *powers, float l, in
 // The weight to 2^-21 of itself (the power on the SFU 2^-22, its argument as a pair of numbers), of finite l.
 template <bool kInexact>
 SPADE_DEVICE float weight_about(const Row &w, float l) {
-  const float s = l - w.m;
+  const float s = fmaf(l, w.scale, -w.m);
   const float ph = s * w.ch;
   float pl = fmaf(s, w.ch, -ph) + s * w.cl;
   if constexpr (kInexact) {  // (the difference of two 16-bit numbers is off only where its weight is nothing)
-    const float back = s - l;
-    pl = fmaf((l - (s - back)) + (-w.m - back), w.ch, pl);
+    const float x = l * w.scale, back = s - x;
+    pl = fmaf((x - (s - back)) + (-w.m - back), w.ch, pl);
   }
   const float q = ex2(ph);
   return s == 0.f ? 1.f : ph > -120.f ? fmaf(q * pl, 0.693147181f, q) : 0.f;
@@ -265,7 +269,8 @@ struct Shared {
   int cut;
   int cuts[2];               // a round of histograms' boundary bin, and what is above it: by turns, as a thread late in
   Mass above[2];             // reading one round's must not find the next round's
-  float ch, cl, tau;         // log2(e) / T, high and low part
+  float ch, cl, scale, tau;  // see Row
+  float u, top_p, temp;      // options, for the code after the loops that need the registers
 };
 
 // What a block's threads need for the meetings of its cluster.
@@ -443,7 +448,7 @@ SPADE_DEVICE uint32_t reach(const Team &team, R rank, M mass, uint64_t goal, uin
 // bound leaves; each is found by comparing each token with each (n^2: 100 tokens 1 us) or by bisection (n log: 1000
 // tokens about 4 us, where a sort took 20).
 template <class T>
-SPADE_DEVICE void decide(const Params &p, Shared &s, Team &team, const Row &w, uint64_t *keys, uint64_t *mass, int n,
+SPADE_DEVICE void decide(const Params &p, Shared &s, Team &team, const Row &w, float peak, uint64_t *keys, uint64_t *mass, int n,
                          uint64_t out_mass, float bound, const uint8_t *row, int r, int k, float top_p, float u, float tau,
                          bool has_k, bool has_p, bool has_m, float *probs) {
   const int tid = team.tid;
@@ -461,7 +466,7 @@ SPADE_DEVICE void decide(const Params &p, Shared &s, Team &team, const Row &w, u
     own[e] = i < n ? weight<kListShift>(w, powers, number_of(~order[e])) : 0;
   }
   // Orders of listed tokens, without the bits that the type's numbers share.
-  const uint32_t least = ~order_of(w.m) >> T::kSpare, most_order = ~order_of(bound) >> T::kSpare;
+  const uint32_t least = ~order_of(peak) >> T::kSpare, most_order = ~order_of(bound) >> T::kSpare;
   auto rank = [&](int e) { return order[e] >> T::kSpare; };
   auto weight_of = [&](int e) { return own[e]; };
   uint64_t larger = 0;  // with few tokens, one to a thread: the mass of those with a larger logit, and their number
@@ -662,12 +667,18 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
   const bool greedy = temp == 0.f;
   const bool has_k = k < p.V, has_p = top_p < 1.f, has_m = min_p > 0.f;
   if (tid < 256) s.powers[tid] = kPowers.v[tid];
+  if (tid == 0) {
+    s.u = u;
+    s.top_p = top_p;
+    s.temp = temp;
+  }
   if (tid == kThreads - 1 && !greedy) {
     // log2(e) / T as a pair of numbers, the quotient and what it leaves; how far min_p reaches.
     constexpr float kLog2e = 1.44269502162933349609f, kLog2eLow = 1.92596299112661746887e-8f;
-    const float q = __fdiv_rn(kLog2e, temp);
+    s.scale = temp >= kHuge ? 1.f / kHuge : 1.f;
+    const float t = temp * s.scale, q = __fdiv_rn(kLog2e, t);
     s.ch = q;
-    s.cl = q <= FLT_MAX ? __fdiv_rn(__fmaf_rn(-q, temp, kLog2e) + kLog2eLow, temp) : 0.f;
+    s.cl = q <= FLT_MAX ? __fdiv_rn(__fmaf_rn(-q, t, kLog2e) + kLog2eLow, t) : 0.f;
     if (has_m) s.reach = static_cast<double>(temp) * log(static_cast<double>(min_p));
   }
   if (!mbar_wait_unabortable(&s.bar, 0)) atomicOr(p.status, SPADE_DEV_TIMEOUT);
@@ -685,14 +696,13 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
     const uint32_t hi = max(static_cast<uint32_t>(x >> 32), static_cast<uint32_t>(y >> 32));
     return static_cast<uint64_t>(hi) << 32 | max(static_cast<uint32_t>(x), static_cast<uint32_t>(y));
   });
-  Row w;
-  w.m = number_of(static_cast<uint32_t>(ends >> 32));
+  const float peak = number_of(static_cast<uint32_t>(ends >> 32));
   float *probs = p.probs ? p.probs + static_cast<int64_t>(r) * p.V : nullptr;
   auto number = [&](int x) {  // token x of this part
     const int i = x - first;
     return T::number(s_vec[i / E], i % E);
   };
-  if (ends >> 32 == 0xffffffffull || w.m == -INFINITY) {
+  if (ends >> 32 == 0xffffffffull || peak == -INFINITY) {
     // Nothing to draw from.
     if (team.rank == 0 && tid == 0) {
       p.tokens[r] = -1;
@@ -707,12 +717,12 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
 
   if (greedy) {
     uint64_t at = 0xffffffffull;
-    if (top == w.m)
+    if (top == peak)
       for (int i = tid; i < n_vec && at == 0xffffffffull; i += kThreads) {
         const uint4 x = s_vec[i];
 #pragma unroll
         for (int e = E - 1; e >= 0; --e)
-          if (T::number(x, e) == w.m) at = first + i * E + e;
+          if (T::number(x, e) == peak) at = first + i * E + e;
       }
     at = team.cluster(at, [](uint64_t x, uint64_t y) { return x < y ? x : y; });
     if (team.rank == 0 && tid == 0) {
@@ -723,13 +733,16 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
       for (int x = lo_x + tid; x < hi_x; x += kThreads) probs[x] = x == static_cast<int>(at) ? 1.f : 0.f;
     return;
   }
+  Row w;
+  w.scale = s.scale;
+  w.m = peak * w.scale;
   w.ch = s.ch;
   w.cl = s.cl;
   const uint64_t *powers = s.powers;
   // The least logit that min_p keeps: ln(min_p) T above the largest, rounded up to fp32.
   float tau = -FLT_MAX;
   if (has_m) {
-    if (tid == 0) s.tau = __double2float_ru(static_cast<double>(w.m) + s.reach);
+    if (tid == 0) s.tau = __double2float_ru(static_cast<double>(peak) + s.reach);
     __syncthreads();
     tau = fmaxf(tau, s.tau);
   }
@@ -743,9 +756,9 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
       float bound = by_min_p ? tau : -FLT_MAX;
       bool whole_set = true;  // every token that can be kept is listed
       if (attempt && p.V > kLocal && (has_k || has_p)) {
-        const float range = w.m - number_of(~static_cast<uint32_t>(ends));
+        const float range = peak - number_of(~static_cast<uint32_t>(ends));
         const float scale = static_cast<float>(kBins) / range;
-        if (top > -INFINITY) atomicAdd(&s.hist[static_cast<int>(fminf((w.m - top) * scale, static_cast<float>(kBins - 1)))], 1u);
+        if (top > -INFINITY) atomicAdd(&s.hist[static_cast<int>(fminf((peak - top) * scale, static_cast<float>(kBins - 1)))], 1u);
         if (tid == 0) s.cut = kBins;
         cluster_sync();
         // Every CTA adds up all parts' bins and finds the same cut.  A nucleus: as many threads as have kAim tokens
@@ -769,7 +782,7 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
         if (tid < kBins && count >= wanted) atomicMin(&s.cut, tid);
         __syncthreads();
         // (A little lower than the bin's edge, whose tokens it has to let in.)
-        const float edge = w.m - (static_cast<float>(s.cut) + 1.0005f) * (range * (1.f / kBins));
+        const float edge = peak - (static_cast<float>(s.cut) + 1.0005f) * (range * (1.f / kBins));
         if (s.cut < kBins && edge > bound) {
           bound = edge;
           whole_set = false;
@@ -779,7 +792,7 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
       // (A vector's largest number first: few vectors hold a token of the list.)
       float in = 0.f;
       F2 outs[2] = {f2(0.f, 0.f), f2(0.f, 0.f)};
-      const F2 minus_m = f2(-w.m, -w.m), ch = f2(w.ch, w.ch);
+      const F2 scale = f2(w.scale, w.scale), minus_m = f2(-w.m, -w.m), ch = f2(w.ch, w.ch);
 #pragma unroll 2
       for (int i = tid; i < n_vec; i += kThreads) {
         const uint4 x = s_vec[i];
@@ -788,7 +801,7 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
         if (masses) {
 #pragma unroll
           for (int e = 0; e < E; e += 2) {
-            f2_split(f2_mul(f2_add(f2(T::number(x, e), T::number(x, e + 1)), minus_m), ch), q[e], q[e + 1]);
+            f2_split(f2_mul(f2_fma(f2(T::number(x, e), T::number(x, e + 1)), scale, minus_m), ch), q[e], q[e + 1]);
             q[e] = ex2(q[e]);
             q[e + 1] = ex2(q[e + 1]);
           }
@@ -845,7 +858,7 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
       // some forty terms (40 2^-24): below 2^-16 in all; and V weights below 2^-64, and what a warp's sum loses as a
       // whole number.
       const bool enough = whole_set || (has_k ? counts >= static_cast<uint64_t>(k)
-                                              : in_mass - (in_mass >> 15) >= part_of(top_p, in_mass + out_mass + (out_mass >> 15), true));
+                                              : in_mass - (in_mass >> 15) >= part_of(s.top_p, in_mass + out_mass + (out_mass >> 15), true));
       if (counts > kList || !enough) {
         if (tid == 0) s.count = 0;  // (read by all before the cluster met)
         __syncthreads();
@@ -869,7 +882,7 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
         zeros();
         return;
       }
-      decide<T>(p, s, team, w, keys, mass, static_cast<int>(counts), out_mass, bound, row, r, k, top_p, u, tau, has_k, has_p, has_m, probs);
+      decide<T>(p, s, team, w, peak, keys, mass, static_cast<int>(counts), out_mass, bound, row, r, k, s.top_p, s.u, tau, has_k, has_p, has_m, probs);
       return;
     }
   }
@@ -878,10 +891,10 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
     // The largest `g` (an order without the spare bits) such that tokens from it on reach `goal`, in counts or masses;
     // tokens are those from `lo` on, which reach it unless there are too few (then lo).
     auto boundary = [&](uint32_t lo, Mass goal, bool masses) {
-      uint32_t hi = (order_of(w.m) >> T::kSpare) + 1;
+      uint32_t hi = (order_of(peak) >> T::kSpare) + 1;
       Mass above = 0;  // of tokens from hi on
       // First round: bins of equal width, to 24 T below the largest logit (or as far as the threads' largest reach).
-      const float width = fmaxf(fminf(24.f * temp, FLT_MAX), w.m - number_of(~static_cast<uint32_t>(ends))) * (1.f / kBins);
+      const float width = fmaxf(fminf(24.f * s.temp, FLT_MAX), peak - number_of(~static_cast<uint32_t>(ends))) * (1.f / kBins);
       const float scale = __fdiv_rn(1.f, width);
       bool by_value = scale > 0.f && scale <= FLT_MAX;
       for (int turn = 0; hi - lo > 1; turn ^= 1) {
@@ -891,7 +904,7 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
         int shift = 0;
         while ((hi - 1 - lo) >> shift >= kBins) ++shift;
         // Bin b begins at the order top_of(b), the first below the bin before.
-        auto top_of = [&](int b) { return by_value ? order_of(fmaf(static_cast<float>(-b), width, w.m)) >> T::kSpare : hi - 1 - (static_cast<uint32_t>(b) << shift); };
+        auto top_of = [&](int b) { return by_value ? order_of(fmaf(static_cast<float>(-b), width, peak)) >> T::kSpare : hi - 1 - (static_cast<uint32_t>(b) << shift); };
         for (int i = tid; i < n_vec; i += kThreads) {
           const uint4 x = s_vec[i];
 #pragma unroll
@@ -901,7 +914,7 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
             if (g < lo || g >= hi) continue;
             int b;
             if (by_value) {
-              b = static_cast<int>(fminf((w.m - l) * scale, static_cast<float>(kBins - 1)));
+              b = static_cast<int>(fminf((peak - l) * scale, static_cast<float>(kBins - 1)));
               while (b > 0 && g > top_of(b)) --b;
               while (b < kBins - 1 && g <= top_of(b + 1)) ++b;
             } else {
@@ -962,7 +975,7 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
         }
       }
       whole = team.cluster_sum(whole);
-      edge = boundary(edge, part_of(top_p, whole, true), true);
+      edge = boundary(edge, part_of(s.top_p, whole, true), true);
     }
     tau = fmaxf(tau, number_of(edge << T::kSpare));
   }
@@ -1023,7 +1036,7 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
     total = exact ? low_of(all >> (kMassShift - 40)) : low_of(all);
     // A token's end and the target differ by the weights before it times 1 - u less those behind times u: that is off by
     // 2 u (1 - u) <= 1/2 of the weights' errors, 2^-20 and little more of the whole (roundings to units: one a token).
-    const M target = target_of(u, all), margin = exact ? 0 : static_cast<M>((low_of(all) >> 20) + p.V);
+    const M target = target_of(s.u, all), margin = exact ? 0 : static_cast<M>((low_of(all) >> 20) + p.V);
     if (target >= before && target < before + mine) {
       for (int i0 = w0; i0 < w1; i0 += 32) {
         const M m = lane_mass(i0 + lane), upto = before + warp_scan(m, lane);

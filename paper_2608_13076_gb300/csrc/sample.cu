@@ -788,6 +788,8 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const __grid_consta
           whole_set = false;
         }
       }
+      // (The bound that has just listed too many: it would do so again.)
+      if (attempt && by_min_p && whole_set) break;
       // ---- the tokens that reach it; roughly, the mass of those and of the others ----
       // (A vector's largest number first: few vectors hold a token of the list.)
       float in = 0.f;

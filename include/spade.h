@@ -655,7 +655,7 @@ spade_status spade_verify_rope_paged(const void *qkv, int64_t qkv_stride, const 
  * n_draft[b] of its mask.  Masks may be any (a row need not see itself); a row that
  * sees nothing gets zeros and the lse -infinity.  What slots that a row does not see
  * hold, NaN included, does not reach it; a row that sees a value of its block that
- * is not finite is NaN in every dim.
+ * is not finite is NaN in every dim, with the lse of its scores.
  *   tree_mask  int32 [R, mask_words], as above
  *   workspace  at least spade_tree_attn_workspace_size(...) bytes, 256-byte aligned,
  *              ZEROED ONCE (and again after a call that set SPADE_DEV_TIMEOUT);

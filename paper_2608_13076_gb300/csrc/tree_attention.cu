@@ -13,7 +13,7 @@
 //    each stream (D columns).  S(j + 2) follows PV(j), which reads P, in the same in-order pipe.
 //  * K and V tiles by TMA, two stages each.  A warp goes over every V tile that reaches into the block before
 //    its product: rows past the live cache (or not loaded) become zeros, and rows of the block with a value that
-//    is not finite too (those that see them are made NaN through their sums, a step later: the scores do not wait
+//    is not finite too (those that see them are made NaN in the epilogue, noted a step later: the scores do not wait
 //    for the values), as 0 times NaN would reach rows that do not see them.
 //  * Lazy rescaling: a row's maximum moves only when a score exceeds it by more than 2^8 (a vote of the row's two
 //    warps); those then rescale their own lanes of O (their stream's last PV is done when S is).
@@ -239,6 +239,22 @@ SPADE_DEVICE uint32_t seen_word(uint32_t w, int i, int kd) {
   return i < 0 ? 0xffffffffu : left < 0 ? 0u : left < 31 ? w & ((2u << left) - 1) : w;
 }
 
+// A warp's half of the columns of O: NaN in the lanes of `odd` rows.  (Out of line: hardly ever needed.)
+template <int D>
+__device__ __noinline__ void make_nan(uint32_t t_o, bool odd) {
+#pragma unroll 1
+  for (int w = 0; w < D / 32; ++w) {
+    uint32_t o[16];
+    tmem_ld8(t_o + 16 * w, o);
+    tmem_ld8(t_o + 16 * w + 8, o + 8);
+    tmem_wait_ld();
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[e] = odd ? 0x7fffffffu : o[e];
+    tmem_st16(t_o + 16 * w, o);
+  }
+  tmem_wait_st();
+}
+
 // Many parts: a part's O has been written; here its m and l.  The CTA whose part completes a group adds the group up, its sum
 // taking the first part's place, and the one whose group completes the unit adds those up, in their order, for the row
 // `orow` (-1: none).  A part is 64 KB, which a CTA reads in about a microsecond: 1 sequence, 1 KV head of 32000 slots
@@ -341,9 +357,8 @@ __device__ __noinline__ void merge_groups(const Params &p, float m, float l, int
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             const float4 x = acc[2 * e], y = acc[2 * e + 1];
-            dst[e] = l == 0.f ? make_uint4(0, 0, 0, 0)
-                              : make_uint4(pack_bf16(x.x * inv, x.y * inv), pack_bf16(x.z * inv, x.w * inv),
-                                           pack_bf16(y.x * inv, y.y * inv), pack_bf16(y.z * inv, y.w * inv));
+            auto two = [&](float a, float b) { return pack_bf16(fmaf(a, inv, 0.f), fmaf(b, inv, 0.f)); };
+            dst[e] = make_uint4(two(x.x, x.y), two(x.z, x.w), two(y.x, y.y), two(y.z, y.w));
           }
         } else {
 #pragma unroll
@@ -752,6 +767,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int q_row = s_q0[g.b] + node;
       const int32_t *mask = p.mask + static_cast<int64_t>(real ? q_row : s_q0[g.b]) * p.words;
       float m = -INFINITY, l = 0.f;
+      bool odd = false;  // the row sees a value of the block that is not finite: its O becomes NaN, its l is the scores' alone
       // From the step j_tail on, chunks reach into the block.  The words of the row's mask are asked for a step ahead, and
       // what they name of values that are not finite is looked at a step later (the values are there later than the
       // scores): such a row becomes NaN.
@@ -768,7 +784,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t it = it0 + (dual ? j : 2 * j + s);
         if (!mbar_wait(&bars[kBarBad + it % kBadRing], (it / kBadRing) & 1, s_abort)) expired = true;
         const uint32_t *bad = s_bad + 4 * (it % kBadRing) + 2 * half;
-        if ((was[0] & bad[0]) | (was[1] & bad[1])) l = __uint_as_float(0x7fffffffu);
+        if ((was[0] & bad[0]) | (was[1] & bad[1])) odd = true;
       };
       if (j_tail == 0 && mysteps > 0) look(0);
       for (int j = 0; j < mysteps; ++j, ++step) {
@@ -869,9 +885,13 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (busy) {
           // The row's sum over both halves of the keys.
           if (mysteps > j_tail) look_back(mysteps - 1);
-          s_half[half * kRows] = l;
+          // (A sum is not negative: its sign says that the half is odd.)
+          s_half[half * kRows] = odd ? -l : l;
           named_bar(pair, 64);
-          l += s_half[(half ^ 1) * kRows];
+          const float rest = s_half[(half ^ 1) * kRows];
+          l += fabsf(rest);
+          odd |= static_cast<int32_t>(__float_as_uint(rest)) < 0 && rest == rest;
+          if (__any_sync(0xffffffffu, odd)) make_nan<D>(t_o, odd);
         }
       }
       float mine = 1.f, other = 0.f;  // factors of this stream's O and of the other's
@@ -1019,7 +1039,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             uint32_t r[4];
 #pragma unroll
             for (int t = 0; t < 4; ++t)
-              r[t] = L == 0.f ? 0u : pack_bf16(__uint_as_float(o[8 * e + 2 * t]) * inv, __uint_as_float(o[8 * e + 2 * t + 1]) * inv);
+              r[t] = pack_bf16(fmaf(__uint_as_float(o[8 * e + 2 * t]), inv, 0.f), fmaf(__uint_as_float(o[8 * e + 2 * t + 1]), inv, 0.f));
             dst[e] = make_uint4(r[0], r[1], r[2], r[3]);
           }
         }

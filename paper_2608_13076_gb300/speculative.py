@@ -208,7 +208,7 @@ class ToyVerifierTree(ToyVerifier):
         scaling = scaling or {}
         self.inv_freq = rope.inv_freq(c.rope_theta, c.D, device=self.device, **scaling)
         self.mscale = rope.attention_scale(scaling["factor"]) if scaling.get("kind") == "bands" else 1.0
-        self.workspaces = {}
+        self.workspace = None
 
     def _make_cache(self):
         # Pages dealt to the sequences in turn, as a serving pool would end up.
@@ -218,12 +218,13 @@ class ToyVerifierTree(ToyVerifier):
         self.v_pools = torch.zeros_like(self.k_pools)
         self.table = torch.arange(B * max_pages, dtype=torch.int32).reshape(max_pages, B).t().contiguous().to(self.device)
 
-    def _workspace(self, max_k):
+    def _workspace(self):
+        # One for blocks of every size, as its own depends on the head dim alone.
         c = self.cfg
-        if max_k not in self.workspaces:
-            self.workspaces[max_k] = tree_attn_workspace(self.B, c.Hq, c.Hkv, c.D, self.table.shape[1] * self.page, max_k,
-                                                         device=self.device)
-        return self.workspaces[max_k]
+        if self.workspace is None:
+            self.workspace = tree_attn_workspace(self.B, c.Hq, c.Hkv, c.D, self.table.shape[1] * self.page, 0,
+                                                 device=self.device)
+        return self.workspace
 
     def _hidden(self, tokens, parents, kd, cu_q, max_k):
         """The last layer's output at every node; the nodes' keys and values are in the caches' slots from ctx on."""
@@ -239,7 +240,7 @@ class ToyVerifierTree(ToyVerifier):
             spade_verify_rope_paged(x @ self.w_qkv[i].t(), self.inv_freq, pos, self.table, self.ctx, kd, cu_q, q, *kv,
                                     mscale=self.mscale, max_k=max_k, status=self.status)
             spade_verify_attention_tree_paged(q, *kv, self.table, self.ctx, kd, cu_q, mask, out, max_k=max_k,
-                                              workspace=self._workspace(max_k), status=self.status)
+                                              workspace=self._workspace(), status=self.status)
             x = (x.float() + out.reshape(R, c.Hq * c.D).float() @ self.w_o[i].float().t()).to(torch.bfloat16)
         return x
 

@@ -1,0 +1,19 @@
+"""What the tree loop's verifier keeps and sets up (CPU: no kernel is launched)."""
+import torch
+
+from paper_2608_13076_gb300 import speculative as S
+
+
+def test_one_workspace_for_prompts_of_all_lengths(monkeypatch):
+    """A verifier that has met many lengths of prompts and blocks holds one workspace of the attention."""
+    made = []
+    monkeypatch.setattr(S, "tree_attn_workspace", lambda *a, **k: made.append(torch.zeros(8)) or made[-1])
+    used = []
+    monkeypatch.setattr(S, "spade_tree_layout", lambda *a, **k: None)
+    monkeypatch.setattr(S, "spade_verify_rope_paged", lambda *a, **k: None)
+    monkeypatch.setattr(S, "spade_verify_attention_tree_paged", lambda *a, workspace, **k: used.append(workspace))
+    v = S.ToyVerifierTree(S.ToyConfig(), 1, 100, seed=1, device="cpu")
+    for n in (3, 9, 40, 41, 77):
+        kd, cu = torch.tensor([n - 1], dtype=torch.int32), torch.tensor([0, n], dtype=torch.int32)
+        v.write_prefix(torch.arange(n), v.ctx, kd, cu, n - 1)
+    assert len(made) == 1 and len(used) == 5 * v.layers and all(w is made[0] for w in used)

@@ -5,7 +5,9 @@ Pair j of `dims` turning dims turns by theta^(-2j/dims) radians per position.  A
   "linear": every pair by 1 / factor (positions are interpolated);
   "ntk":    theta times factor^(dims / (dims - 2)): the slowest pair by 1 / factor, the fastest as it was;
   "bands":  by the turns r = context * frequency / (2 pi) that a pair makes over the trained context: as it
-            was from r = high on, by 1 / factor up to r = low, linear in r between.
+            was from r = high on, by 1 / factor up to r = low, linear in r between.  The defaults, low 1 and high 4,
+            are those of the Llama-3.1 family, whose turned dims have no factor; others go up to high = 32, with the
+            factor of attention_scale.
 Set-up code in torch; nothing here is on a verify step's path.
 """
 from __future__ import annotations
@@ -39,5 +41,6 @@ def inv_freq(theta, dims, kind=None, factor=1.0, context=None, low=1.0, high=4.0
 
 
 def attention_scale(factor):
-    """The factor of the turned dims that goes with "bands": 0.1 ln(factor) + 1."""
+    """0.1 ln(factor) + 1: the factor of the turned dims (mscale of spade_verify_rope) of models that were stretched with
+    one.  It scales the scores by its square, so it is for a model whose configuration says so, and for no other."""
     return 0.1 * math.log(factor) + 1.0

@@ -194,9 +194,11 @@ class ToyVerifierInt4(ToyVerifier):
 
 class ToyVerifierTree(ToyVerifier):
     """A decoder of `layers` attention layers over paged caches in pages of `page` slots, whose verify blocks are
-    trees.  ``scaling``: how the rotary frequencies are stretched (arguments of rope.inv_freq)."""
+    trees.  ``scaling``: how the rotary frequencies are stretched (arguments of rope.inv_freq); ``mscale``: the factor of
+    the turned dims, where the model has one (rope.attention_scale)."""
 
-    def __init__(self, cfg: ToyConfig, B: int, cap: int, seed: int, device, layers: int = 2, page: int = 64, scaling=None):
+    def __init__(self, cfg: ToyConfig, B: int, cap: int, seed: int, device, layers: int = 2, page: int = 64, scaling=None,
+                 mscale: float = 1.0):
         self.layers, self.page = layers, page
         super().__init__(cfg, B, cap, seed, device)
         c = cfg
@@ -205,9 +207,8 @@ class ToyVerifierTree(ToyVerifier):
             first = getattr(self, name)
             more = [(torch.randn(first.shape, generator=g) * std).to(first) for _ in range(layers - 1)]
             setattr(self, name, torch.stack([first] + more))
-        scaling = scaling or {}
-        self.inv_freq = rope.inv_freq(c.rope_theta, c.D, device=self.device, **scaling)
-        self.mscale = rope.attention_scale(scaling["factor"]) if scaling.get("kind") == "bands" else 1.0
+        self.inv_freq = rope.inv_freq(c.rope_theta, c.D, device=self.device, **(scaling or {}))
+        self.mscale = mscale
         self.workspace = None
 
     def _make_cache(self):

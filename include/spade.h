@@ -658,9 +658,9 @@ spade_status spade_verify_rope_paged(const void *qkv, int64_t qkv_stride, const 
  * is not finite is NaN in every dim, with the lse of its scores.
  *   tree_mask  int32 [R, mask_words], as above
  *   workspace  at least spade_tree_attn_workspace_size(...) bytes, 256-byte aligned,
- *              ZEROED ONCE (and again after a call that set SPADE_DEV_TIMEOUT);
- *              calls of any sizes may share one that is large enough for each,
- *              ordered
+ *              its first SPADE_TREE_ATTN_ZEROED ZEROED ONCE (and again after a
+ *              call that set SPADE_DEV_TIMEOUT); calls of any sizes may share one
+ *              that is large enough for each, ordered
  * Everything else is as for spade_verify_attention and its paged form (pages of a
  * multiple of 64 slots).  The softmax weights are rounded to bf16 (2^-8 of
  * themselves) on their way into the product with the values, sums are fp32.
@@ -679,6 +679,9 @@ spade_status spade_verify_attention_tree_paged(
     void *out, float *lse, int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t page_size,
     int32_t num_pages, int32_t max_pages, int32_t mask_words, int32_t max_k, int32_t R,
     void *workspace, size_t workspace_bytes, int32_t *status, spade_stream_t stream);
+
+/* Bytes at the workspace's start that have to be zero before its first use. */
+#define SPADE_TREE_ATTN_ZEROED 65536
 
 /* Bytes of workspace that the two calls above need for these sizes on the current
  * device (cap: max_pages * page_size for the paged form; 0 on invalid sizes).  They

@@ -56,6 +56,7 @@ DEV_BAD_INDEX = 0x1
 DEV_CAPACITY = 0x2
 DEV_TIMEOUT = 0x4
 DEV_FALLBACK = 0x8
+TREE_ATTN_ZEROED = 65536  # bytes of a tree attention's workspace that are zeroed once
 
 _lib = None
 _native = None  # the extension module, once loaded
@@ -517,12 +518,14 @@ def spade_tree_attn_workspace_size(B, Hq, Hkv, D, cap, max_k):
 
 
 def tree_attn_workspace(B, Hq, Hkv, D, cap, max_k, device="cuda"):
-    """A zeroed workspace for spade_verify_attention_tree (zeroed once; calls keep its counters zeroed).  Calls of other sizes
+    """A workspace for spade_verify_attention_tree whose counters are zero (calls leave them so).  Calls of other sizes
     may use it too, one after the other, if it is large enough for them: its size depends on the head dim alone."""
     n = spade_tree_attn_workspace_size(B, Hq, Hkv, D, cap, max_k)
     if n == 0:
         raise SpadeError(-1, "spade_tree_attn_workspace_size returned 0: " + load().spade_last_error().decode())
-    return torch.zeros(n, dtype=torch.uint8, device=device)
+    ws = torch.empty(n, dtype=torch.uint8, device=device)
+    ws[:TREE_ATTN_ZEROED].zero_()
+    return ws
 
 
 def spade_verify_attention_tree(q, k_cache, v_cache, ctx_lens, n_draft, cu_q, tree_mask, out, lse=None, *, max_k,

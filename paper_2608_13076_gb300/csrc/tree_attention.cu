@@ -1093,7 +1093,8 @@ static spade_status check_sizes(const char *name, int B, int Hq, int Hkv, int D,
 }
 
 // The workspace: counters of split units, those of groups of parts, the parts.  Where the counters lie depends on the device
-// alone, so that calls of all sizes find them as the last call left them, whatever it was.
+// alone, so that calls of all sizes find them as the last call left them, whatever it was.  (SPADE_TREE_ATTN_ZEROED has
+// room for those of 2048 SMs.)
 static size_t counter_bytes(int sms) { return round_up(static_cast<size_t>(sms) * 16, 256); }
 static size_t workspace_bytes_of(int sms, int D) {
   return 2 * counter_bytes(sms) + static_cast<size_t>(sms) * 4 * part_floats(D) * sizeof(float);

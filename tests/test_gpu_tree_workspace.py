@@ -47,3 +47,17 @@ def test_the_size_depends_on_the_head_dim_alone(gpu_lib):
                  ((1, 1, 1, 64, 0), (8, 4, 8, 4608, 511), (512, 8, 8, 1024, 100), (3, 5, 2, 40_000, 2000))}
         assert len(sizes) == 1
 
+
+
+@pytest.mark.parametrize("ctx,k,G,Hkv,D", [([30_000], [5], 4, 1, 128), ([3000, 200], [300, 2], 1, 2, 64)])
+def test_only_the_counters_have_to_be_zero(gpu_lib, ctx, k, G, Hkv, D):
+    """What lies behind them in a new workspace does not matter."""
+    c = T.cache(ctx, k, Hkv, D, 0, 210, DEV)
+    q = T.queries(c, G, 211)
+    mask = T.tree_mask(T.parents(k, "tree", 212), k, c["cu"].cpu())
+    out, lse, st = T.attention(c, q, mask)
+    ws = torch.full_like(gpu_lib.tree_attn_workspace(c["B"], G * Hkv, Hkv, D, c["cap"], c["max_k"]), 255)
+    ws[:gpu_lib.TREE_ATTN_ZEROED] = 0
+    got, l2, st2 = T.attention(c, q, mask, workspace=ws)
+    assert int(st.item()) == int(st2.item()) == 0
+    assert torch.equal(got, out) and torch.equal(l2, lse)

@@ -46,7 +46,8 @@ struct Params {
 // cache.  An out-of-range page id is reported and mapped past the last row,
 // where the tensor copy reads zeros.  (A plain load: the kernels are launched while the one
 // before still runs, and a read-only load promises that nothing writes its data meanwhile.)
-__device__ __forceinline__ int paged_row(const Params &p, int b, int kvh, int key) {
+template <class P>
+__device__ __forceinline__ int paged_row(const P &p, int b, int kvh, int key) {
   const int page = p.block_table[static_cast<int64_t>(b) * p.max_pages + key / p.page_size];
   const int64_t rows = static_cast<int64_t>(p.num_pages) * p.Hkv * p.page_size;
   if (page < 0 || page >= p.num_pages) {

@@ -37,6 +37,7 @@ namespace attn_tree {
 using attn::block_sync;
 using attn::desc_sw128;
 using attn::named_bar;
+using attn::paged_row;
 
 constexpr int kKeys = 128;                    // keys per chunk
 constexpr int kRows = 128;                    // rows per tile
@@ -212,16 +213,6 @@ struct Sched {
     return s;
   }
 };
-
-// Pool row of the 64 keys from `key` on (see attn::paged_row).
-SPADE_DEVICE int paged_row(const Params &p, int b, int kvh, int key) {
-  const int page = p.block_table[static_cast<int64_t>(b) * p.max_pages + key / p.page_size];
-  if (page < 0 || page >= p.num_pages) {
-    atomicOr(p.status, SPADE_DEV_BAD_INDEX);
-    return static_cast<int>(static_cast<int64_t>(p.num_pages) * p.Hkv * p.page_size);
-  }
-  return static_cast<int>((static_cast<int64_t>(page) * p.Hkv + kvh) * p.page_size + key % p.page_size);
-}
 
 // Not 0 if one of the eight bf16 numbers is not finite.
 SPADE_DEVICE uint32_t times_zero(const uint4 &v) {

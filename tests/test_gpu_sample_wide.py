@@ -49,3 +49,20 @@ def test_a_uniform_beside_an_edge_at_a_huge_temperature(gpu_lib, probs):
         want = int(mass / w * (V // 2)) if mass < w else V // 2 + int((mass - w) * (V // 2))
         tok, _, _, st = call(gpu_lib, x, u, temperature=t, probs=probs)
         assert st == 0 and int(tok[0]) == want
+
+
+@pytest.mark.parametrize("temperature", [1e-45, 1e-39, 1.2e-38])
+@pytest.mark.parametrize("opts", [dict(), dict(top_p=0.7), dict(top_p=0.99999), dict(top_k=9), dict(min_p=0.3)], ids=str)
+@pytest.mark.parametrize("V", [900, 32003])
+def test_the_smallest_temperatures(gpu_lib, V, temperature, opts):
+    """Down to where log2(e) / T is no finite number: equal largest logits share the mass, all others have none."""
+    gen = torch.Generator().manual_seed(V)
+    x = torch.randn((4, V), generator=gen)
+    x[1, ::7] = x[1].max()
+    x[2] = 1.5
+    x[3, 5] = x[3].max() * (1 + 2.0 ** -20)
+    x, u, t = x.to(DEV), uniforms(4, V + 2), float(np.float32(temperature))
+    for probs in (True, False):
+        tok, pr, ch, st = call(gpu_lib, x, u, temperature=t, probs=probs, **opts)
+        assert st == 0
+        check(x, u, tok, pr, ch, temperature=t, loose=2.0 ** -21 if probs else 2.0 ** -20 + 2.0 ** -21, **opts)

@@ -629,7 +629,7 @@ spade_status spade_tree_layout(const int32_t *parents, const int32_t *ctx_lens,
  *   q_out      bf16 [R, Hq, D]
  *   status     as for spade_verify_qkv_rope: a block that is invalid or does not fit
  *              is skipped; a slot whose page is not in the pool is not written
- * Angles are reduced in 64 bits: a position of 2^31 turns as exactly as a near one.
+ * Angles are reduced in 64 bits: to 2^-24 of a turn at positions of 2^31.
  * R has no upper limit; head dims 64 and 128.
  */
 spade_status spade_verify_rope(const void *qkv, int64_t qkv_stride, const double *inv_freq,

@@ -56,16 +56,16 @@ SPADE_DEVICE int sequence_of(const Params &p, int row, int lane, int *ctx, int *
 }
 
 // One CTA per row.  Its angles (rot / 2 of them) are made once and shared by all heads: the position
-// times frequency / 2 pi in 64 bits, so that the turns that are dropped cost nothing at far
-// positions, then sincospif of the rest in fp32 (2^-25 of a turn).  A head's D dims lie on D / 8
+// times frequency / 2 pi in 64 bits, so that the turns that are dropped cost next to nothing at far
+// positions (2^-24 of a turn at 2^31), then sincospif of the rest in fp32 (2^-25 of a turn).  A head's D dims lie on D / 8
 // lanes, eight neighbours each; in the half layout the rotation's partner is rot / 16 lanes away.
 // The heads' loads are issued before all else, and the last threads make the angles while the first
 // look for the row's sequence.  A lane's angles lie a lane's width apart in shared memory, where the
 // lanes of a warp read neighbours (eight next to each other per lane met the same banks: 1376 rows of
 // 56 heads 14.2 us instead of 9.1).
 // Bound by the bytes where rows are many: a row's heads once in, once out (12288 rows of 48 heads of
-// 128: 47 us, 6.4 TB/s; 1376 of 56 9.1 us, 4.3 TB/s), by latency where they are few (512 rows of 48
-// heads 3.7 us; 3.9 with one product at a time instead of two).  Five CTAs of 256 threads to an SM: with six,
+// 128: 47 us, 6.4 TB/s; 1376 of 56 9.1 us, 4.3 TB/s, in a step of several layers and 10 alone; 4096 rows of 512
+// sequences 22, 4.6 TB/s), by latency where they are few (512 rows of 48 heads 3.7 us; 3.9 with one product at a time instead of two).  Five CTAs of 256 threads to an SM: with six,
 // 1376 rows 9.5 us, with seven 11.2; two or eight vectors a thread were slower as well, and angles in registers.
 constexpr int kVecs = 4;  // 16-byte vectors of a thread in flight
 constexpr int kMaxThreads = 256;

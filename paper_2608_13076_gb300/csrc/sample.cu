@@ -23,8 +23,8 @@
 // those do not settle the token.
 //
 // Measured, back to back (in brackets the time in which the logits, and probabilities, pass HBM once): 8 rows of 128256 fp32
-// with top-k, top-p and probabilities 14.1 us (1.2), 512 rows in bf16 with top-p and min-p 80 (19), with top-p alone
-// 136, with top-k 71, greedy 37, with nothing to leave out 103.  Few rows are bound by the meetings of the cluster and
+// with top-k, top-p and probabilities 14.4 us (1.2), 512 rows in bf16 with top-p and min-p 81 (19), with top-p alone
+// 139, with top-k 72, greedy 38, with nothing to leave out 97; nuclei of tens of thousands of tokens 820.  Few rows are bound by the meetings of the cluster and
 // of the deciding CTA's threads (about a microsecond each, 14 of them), many by the same on 456 CTAs at a time: a
 // part's 51 KB are there after 1 of its 15 us.  384 threads, three CTAs to an SM: 256 and four take 77 us for the 512
 // rows with top-p and min-p, but 46 instead of 41 for 72 rows with top-p; 512 and two 82 and 55.

@@ -26,8 +26,9 @@ struct Layout {
 // One CTA per sequence.  Nodes are taken in blocks of 32, a warp's lanes: within its block a
 // node's ancestors are found by five doublings of the path (bits |= bits[up], up = up[up]) in
 // registers; what is left is the first ancestor in an earlier block, so the walk to the root
-// takes one step per block that the path meets, not one per node.  Latency is all there is: 8
-// trees of 64 nodes (8 KB) 1.5 us, 64 of up to 512 (1.4 MB, 0.2 us of HBM) 3.7 us.
+// takes one step per block that the path meets, not one per node.  Latency is all there is, in a
+// graph 1.6 us for 8 trees of 64 nodes (8 KB) and 3.8 for 64 of up to 512 (1.4 MB, 0.2 us of HBM);
+// calls from the host take 3.1 and 4.0.
 __global__ void __launch_bounds__(kThreads) layout_kernel(const __grid_constant__ Layout p, int nodes) {
   extern __shared__ int32_t smem[];
   uint32_t *s_bits = reinterpret_cast<uint32_t *>(smem);  // [nodes] ancestors within the node's block
@@ -114,8 +115,8 @@ struct Commit {
 // block's rows in its planes.  Rows of the path move to lower slots in order, a thread per 16-byte
 // column, so that no row is overwritten before it has been read; the barrier between moving and
 // clearing is the CTA's own, as planes are not shared.  (Walking again in every CTA takes no
-// longer than a second launch would.)  8 x 64 nodes, one layer 3.6 us, of which the bytes 0.5; 8
-// layers of 64 x 21 nodes (42 MB, mostly zeros) 11.7, of which 6.3.
+// longer than a second launch would.)  8 x 64 nodes, one layer 3.8 us, of which the bytes 0.5; 8
+// layers of 64 x 21 nodes (42 MB, mostly zeros) 14.1, of which 6.3 (three sets of caches in turn).
 __global__ void __launch_bounds__(kThreads) commit_kernel(const __grid_constant__ Commit p, int nodes) {
   extern __shared__ int32_t smem[];
   int32_t *s_next = smem;               // [nodes] accepted child

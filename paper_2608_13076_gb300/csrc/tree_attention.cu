@@ -23,8 +23,9 @@
 //    number; the last one waits for those before it to be written.  What those still wait for is their own CTA's
 //    products at most, which wait for no other CTA, so the wait ends.)
 //    More than kMany parts are written, added up in groups by as many CTAs, and then the groups (nothing waits there).
-// Measured (bf16, back to back; D = 128): 8 x 64 nodes x 4 heads over 4096 slots 44 us (its keys and values once: 21),
-// 64 ragged ones over 0 .. 8192 slots 208 (163), 2 x 512 nodes x 8 heads over 16384 372 (products at the tensor rate: 292).
+// Measured (bf16, back to back; D = 128): 8 x 64 nodes x 4 heads over 4096 slots 45 us (its keys and values once: 21),
+// 64 ragged ones over 0 .. 8192 slots 214 (163), 2 x 512 nodes x 8 heads over 16384 410-417 (386 in runs of a few
+// milliseconds, where the clock is higher; products at the tensor rate: 292).
 // Long contexts of few nodes are bound by HBM; many rows by a stream's chain: scores from tensor memory, maximum, 64
 // powers and their packing a thread, about 1650 cycles for a tile step, against 1070 of the products; few chunks by
 // the start and the end of a unit, whose code is fetched anew each time.
@@ -153,8 +154,8 @@ SPADE_DEVICE bool await_parts(const int32_t *counter, int n) {
   return false;
 }
 
-// warp_wait with its long part out of line: the loops that wait a few times a step stay short (2 x 512 nodes over 16384 slots 372
-// us, 381 with all of it in its place; with the first try out of line as well 374).
+// warp_wait with its long part out of line: the loops that wait a few times a step stay short (2 x 512 nodes over 16384 slots, in
+// short runs, 372 us; 381 with all of it in its place; with the first try out of line as well 374).
 __device__ __noinline__ bool wait_long(uint64_t *bar, uint32_t parity, volatile int *abort) { return warp_wait(bar, parity, abort); }
 SPADE_DEVICE bool wait_short(uint64_t *bar, uint32_t parity, volatile int *abort) {
   return __all_sync(0xffffffffu, mbar_test_wait(bar, parity)) || __all_sync(0xffffffffu, mbar_try_wait(bar, parity)) ||

@@ -107,10 +107,10 @@ typedef enum {
  *               (SPADE_DEV_CAPACITY) is skipped; none of its rows is written
  *   workspace   device scratch of at least spade_qkv_workspace_size(R, Hq, Hkv, D)
  *               bytes, 256-byte aligned, ZEROED ONCE by the caller after
- *               allocation; every call that completes leaves its counters
- *               zeroed again (a call that reported SPADE_DEV_TIMEOUT may not:
- *               zero the workspace again before the next one).  Calls that
- *               share a workspace must be ordered.
+ *               allocation; every call that completes leaves it ready for the
+ *               next, of any sizes it is large enough for (a call that reported
+ *               SPADE_DEV_TIMEOUT may not: zero the workspace again before the
+ *               next one).  Calls that share a workspace must be ordered.
  * Every pointer is a 16-byte aligned device pointer.  The contraction is split
  * over every SM and its parts' fp32 sums are added in a fixed order, so results
  * do not depend on timing.  Up to 128 rows, and up to 464 over wide layers, two

@@ -59,7 +59,9 @@ constexpr int kMaxStages = 8;
 struct Params {
   Call c;
   float *partials;         // [num_ctas + tiles slots][Ncols][128] fp32 (workspace)
-  int32_t *counters;       // [2][tiles]: parts published, slabs done; zero between calls (workspace)
+  // Of the split tile that begins in a CTA's range (its last one at most): parts published, slabs done.  [SMs] each, zero
+  // between calls, at the workspace's start whatever a call's sizes are.
+  int32_t *published, *slabs_done;
   int tiles;    // (Hq + 2 Hkv) D / 128
   int KC;       // k-chunks (ceil(H / 64))
   int KG;       // k-chunks per ring stage at most (1 or 2; 2 only when H is a multiple of 64)
@@ -383,10 +385,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int nparts = unit_owner(p.units, p.num_ctas, (t + 1) * p.KC - 1) - c_first + 1;
       epi_bar();
       if (nparts > 1 && p.slabs > 1) {
-        if (et == 0) publish_part(&p.counters[t]);
+        if (et == 0) publish_part(&p.published[c_first]);
       } else {
         // Release publishes this part; for the last one, acquire makes the others visible.
-        if (et == 0) *s_last = nparts == 1 || add_acq_rel(&p.counters[t], 1) == nparts - 1;
+        if (et == 0) *s_last = nparts == 1 || add_acq_rel(&p.published[c_first], 1) == nparts - 1;
         epi_bar();
         if (*s_last) {
           if (se == u1) {
@@ -396,7 +398,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               reduce_tile<6, 1>(p, s_row, s_rpos, s_freq, t, c_first, 1, 0, p.c.R, et, kEpiThreads);
             else
               reduce_tile<3, 3>(p, s_row, s_rpos, s_freq, t, c_first, nparts, 0, p.c.R, et, kEpiThreads);
-            if (et == 0 && nparts > 1) p.counters[t] = 0;  // every part has arrived: reset for the next call
+            if (et == 0 && nparts > 1) p.published[c_first] = 0;  // every part has arrived: reset for the next call
           }
         }
       }
@@ -413,13 +415,12 @@ __global__ void __launch_bounds__(kThreads, 1)
       reduce_tile<6, 1>(p, s_row, s_rpos, s_freq, t, c_first, 1, 0, p.c.R, tid, kThreads);
     else
       reduce_tile<3, 3>(p, s_row, s_rpos, s_freq, t, c_first, nparts, 0, p.c.R, tid, kThreads);
-    if (tid == 0 && nparts > 1) p.counters[t] = 0;  // every part has arrived: reset for the next call
+    if (tid == 0 && nparts > 1) p.published[c_first] = 0;  // every part has arrived: reset for the next call
   }
   // Row slabs of the split tiles (slabs > 1): item i = t * slabs + s goes to
   // CTA i mod num_ctas.  The slab waits until all of the tile's parts are
   // published (acquire, bounded), and the tile's last slab to finish resets
   // both counters for the next call.
-  int32_t *published = p.counters, *slabs_done = p.counters + p.tiles;
   for (int item = blockIdx.x; p.slabs > 1 && item < p.tiles * p.slabs; item += p.num_ctas) {
     const int t = item / p.slabs, sl = item - t * p.slabs;
     const int c_first = unit_owner(p.units, p.num_ctas, t * p.KC);
@@ -427,9 +428,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (nparts == 1) continue;  // a whole tile: finished by its CTA
     if (tid == 0) {
       s_fin[3] = 1;
-      if (load_acquire(&published[t]) != nparts) {
+      if (load_acquire(&p.published[c_first]) != nparts) {
         const uint64_t t0 = globaltimer();
-        while (load_acquire(&published[t]) != nparts) {
+        while (load_acquire(&p.published[c_first]) != nparts) {
           if (*s_abort || globaltimer() - t0 > kWaitLimitNs) {  // (later slabs do not wait again)
             *s_abort = 1;
             atomicOr(p.c.status, SPADE_DEV_TIMEOUT);
@@ -447,9 +448,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       reduce_tile<2, 6>(p, s_row, s_rpos, s_freq, t, c_first, nparts, r0, r1, tid, kThreads);
     }
     __syncthreads();  // every load of the parts is done
-    if (tid == 0 && ok && add_acq_rel(&slabs_done[t], 1) == p.slabs - 1) {
-      published[t] = 0;
-      slabs_done[t] = 0;
+    if (tid == 0 && ok && add_acq_rel(&p.slabs_done[c_first], 1) == p.slabs - 1) {
+      p.published[c_first] = 0;
+      p.slabs_done[c_first] = 0;
     }
   }
   tc_fence_before();
@@ -469,10 +470,10 @@ struct Paging {
   const int32_t *block_table;
   int page_size, max_pages, num_pages;
 };
-static size_t counter_bytes(int tiles) { return round_up(static_cast<size_t>(tiles) * 8, 256); }
+static size_t counter_bytes(int sms) { return round_up(static_cast<size_t>(sms) * 8, 256); }
 static size_t workspace_bytes_for(int R, int tiles, int sms) {
   const size_t ncols = static_cast<size_t>((R + 15) / 16 * 16);
-  return counter_bytes(tiles) + static_cast<size_t>(sms + tiles) * ncols * kTileM * 4;
+  return counter_bytes(sms) + static_cast<size_t>(sms + tiles) * ncols * kTileM * 4;
 }
 }  // namespace qkv
 }  // namespace spade
@@ -535,8 +536,9 @@ static spade_status qkv_rope_impl(const void *x, const void *w_qkv, const int32_
   c.num_pages = pg ? pg->num_pages : 0;
   for (int j = 0; j < D / 2; ++j) c.inv_freq[j] = static_cast<float>(pow(static_cast<double>(rope_theta), -2.0 * j / D));
   if (cluster_fits(c, sms)) return launch_cluster(c, x, w_qkv, sms, reinterpret_cast<cudaStream_t>(stream));
-  p.counters = static_cast<int32_t *>(workspace);
-  p.partials = reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + counter_bytes(tiles));
+  p.published = static_cast<int32_t *>(workspace);
+  p.slabs_done = p.published + sms;
+  p.partials = reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + counter_bytes(sms));
   p.tiles = tiles;
   p.KC = (H + kKChunk - 1) / kKChunk;
   p.Ncols = (R + 15) / 16 * 16;
